@@ -41,7 +41,7 @@ extern "C" {
 /* Version of this interface: raised with every change to a declaration
  * below.  cb_abi_version() returns the value the library was built with;
  * a caller built against another version must not call anything else. */
-#define CB_ABI_VERSION 3
+#define CB_ABI_VERSION 4
 int cb_abi_version(void);
 
 typedef struct cb_ctx cb_ctx;
@@ -388,6 +388,125 @@ int cb_test_conv_static(int k, int b, int Ci, int H, int W, int Co, int R, int s
                         int64_t pstride, float* y, double* stats, const float* dy, float* dx,
                         float* grads, void* stream);
 
+/* --- operators for language-model learners -------------------------------
+ * The ends of a transformer block and of the network for k co-resident
+ * learners: the loss over a large vocabulary, the norms around a block, and
+ * activations kept in 8 bits.  Every activation is [k*n][width]: learner j
+ * owns rows (tokens) [j*n, (j+1)*n); parameters and their gradients are
+ * those of learner 0 and a stride in elements to the next learner's, so
+ * that they can lie in flat parameter and gradient vectors.
+ *   - type: CB_TYPE_*, the type of activations, weights, gates and their
+ *     gradients.  Norm gammas and their gradients, losses and log-sum-exps
+ *     are fp32.  Sums are fp32 or wider; each result is rounded once.
+ *   - Pointers are device memory of the device that is current at the call
+ *     and that `stream` (a hipStream_t, NULL = the default stream) belongs
+ *     to, aligned to their element; the workspace to 256 bytes, 8-bit
+ *     buffers to 16.  Outputs must not overlap inputs unless stated.
+ *   - Workspaces are the caller's, of at least the *_workspace_bytes size
+ *     for the same description (0 bytes from those calls: bad description);
+ *     they carry nothing from one call to the next.  Calls that may overlap
+ *     in time need one each.
+ *   - Nothing is allocated and nothing waits: the calls may be captured
+ *     into a graph.  Results do not depend on timing (no atomics).
+ *   - CB_EINVAL for a description out of range, a NULL or misaligned
+ *     pointer, CB_ENOMEM for a short workspace, CB_EDEVICE if a launch
+ *     fails; cb_last_error(NULL) has the message. */
+enum { CB_TYPE_FLOAT = 0, CB_TYPE_HALF = 1, CB_TYPE_BFLOAT = 2 };
+
+/* Softmax cross-entropy of the logits h W^T over v words, from the hidden
+ * rows; logits are never stored.  A row whose label is `ignore` does not
+ * count: whatever h holds there (NaN too) has no effect, its lse is 0 and
+ * its dh 0.  Any other label outside [0, v) makes the learner's loss NaN
+ * and contributes no one-hot term, as in cb_step. */
+typedef struct {
+  int32_t type;
+  int32_t k, n, d, v;    /* d <= 2^20; k*n and v <= 2^30 */
+  int32_t ignore;
+  const void* h;         /* [k*n] rows of d, ldh elements apart */
+  int64_t ldh;
+  const void* w;         /* [v][d] */
+  int64_t pstride;       /* to the next learner's */
+  const int32_t* labels; /* [k*n] */
+} cb_vocab_xent;
+
+/* Workspace of the forward, or with backward != 0 of the backward call.
+ * The forward's holds the counted rows and one pair of floats for each row
+ * and 64 to 128 words; the backward's also the logit gradients of one piece
+ * of the vocabulary (256 MB or 4096 words, whichever is more) and fp32 sums
+ * of dh.  Where rows of w do not start on 16 bytes it holds a copy of w. */
+size_t cb_vocab_xent_workspace_bytes(const cb_vocab_xent* x, int backward);
+
+/* loss [k]: the mean over each learner's counted rows of
+ * lse - logit[label] (0 if none counts); lse [k*n]: log sum exp. */
+int cb_vocab_xent_fwd(const cb_vocab_xent* x, float* loss, float* lse, void* workspace_dev,
+                      size_t ws_bytes, void* stream);
+
+/* The gradients of grad_scale * loss, given the forward's lse: dh [k*n][d],
+ * dw [v][d] with dstride elements to the next learner's (overwritten; all
+ * zero for a learner with no counted row). */
+int cb_vocab_xent_bwd(const cb_vocab_xent* x, const float* lse, float grad_scale, void* dh,
+                      void* dw, int64_t dstride, void* workspace_dev, size_t ws_bytes,
+                      void* stream);
+
+/* The norm after a block, its gate and residual scale, the addition to the
+ * residual stream and the norm before the next block.  With
+ * rms(v) = v / sqrt(mean(v^2) + eps) over a row:
+ *   x_out = x + res_scale * gate * (post * rms(block))
+ *   y     = pre * rms(x_out)
+ * Each part may be left out: block NULL (then gate and post too): x_out is x
+ * and is not written; gate NULL: 1; post NULL: block without a norm; pre
+ * NULL: no y.  Row r of a learner takes row r / gate_rows of its
+ * ceil(n / gate_rows) gate rows: gate_rows 1 is a gate for every element,
+ * n or more one vector for all rows. */
+typedef struct {
+  int32_t type;
+  int32_t k, n, d;       /* d <= 16384, k*n <= 2^30 */
+  int32_t gate_rows;     /* >= 1; not read without a gate */
+  float res_scale, eps;  /* eps > 0 */
+  const void* block;     /* [k*n][d] */
+  const void* gate;      /* [k][ceil(n/gate_rows)][d] */
+  const float* post;     /* [d], post_stride to the next learner's */
+  const float* pre;      /* [d] */
+  int64_t post_stride, pre_stride;
+} cb_gated_norm;
+
+/* y_kept (may be NULL; needs pre): y also in 8 bits, exactly as
+ * cb_ckpt_pack gives it, cb_ckpt_bytes(k*n, d) bytes.  x_out may be x. */
+int cb_gated_norm_fwd(const cb_gated_norm* g, const void* x, void* x_out, void* y, void* y_kept,
+                      void* stream);
+
+/* Workspace of the backward call (the forward needs none). */
+size_t cb_gated_norm_workspace_bytes(const cb_gated_norm* g);
+
+/* Backward, given the forward's x_out (x without a block), dy = the gradient
+ * at y (NULL if and only if pre is) and dres = the gradient that reaches
+ * x_out along the stream (NULL: none): dx = the gradient at x (and at x_out),
+ * dblock, dgate [k][ceil(n/gate_rows)][d] (each the sum over the rows that
+ * share it), dpost and dpre [d] with their strides.  Gradients of parts that
+ * are left out are not written and may be NULL.  dx may be dres or dy. */
+int cb_gated_norm_bwd(const cb_gated_norm* g, const void* x_out, const void* dy, const void* dres,
+                      void* dx, void* dblock, void* dgate, float* dpost, int64_t dpost_stride,
+                      float* dpre, int64_t dpre_stride, void* workspace_dev, size_t ws_bytes,
+                      void* stream);
+
+/* Activations in 8 bits: every 32 neighbouring columns of a row (the last
+ * group may be short) become whole multiples, -127 to 127, of a power of
+ * two, the least that reaches the largest of them; ties round to even.  Each
+ * value is off by at most half that power.  The power is at least 2^-126
+ * (fp16: 2^-24); next to the type's largest finite value multiples stop at
+ * 63, so that nothing unpacks to infinity.  A group with an infinity or NaN
+ * unpacks to NaN.  d <= 2^20, rows <= 2^30. */
+size_t cb_ckpt_bytes(int64_t rows, int d); /* 1.03 bytes a value; 0: bad size */
+int cb_ckpt_pack(int type, int64_t rows, int d, const void* x, void* kept, void* stream);
+int cb_ckpt_unpack(int type, int64_t rows, int d, const void* kept, void* x, void* stream);
+
+/* The weight gradient of a linear layer whose input was kept in 8 bits:
+ * dw[o][c] = sum over the learner's n rows of dy[r][o] * unpacked[r][c], as
+ * [out][d] with dstride elements to the next learner's (overwritten). */
+size_t cb_ckpt_wgrad_workspace_bytes(int type, int k, int n, int d, int out);
+int cb_ckpt_wgrad(int type, int k, int n, int d, int out, const void* kept, const void* dy,
+                  void* dw, int64_t dstride, void* workspace_dev, size_t ws_bytes, void* stream);
+
 /* --- instrumentation --------------------------------------------------- */
 
 /* While enabled, every kernel launch of the context carries a start/stop
@@ -415,7 +534,8 @@ int cb_profile_clear(cb_ctx* c);
 
 /* Message for the last error on this context ("" if none); valid until the
  * next call on it.  A NULL context gives the last failure of a call made
- * without one (cb_create, cb_test_conv_static). */
+ * without one (cb_create, cb_test_conv_static, the language-model
+ * operators). */
 const char* cb_last_error(const cb_ctx* c);
 
 /* Frees the context's host-side state; the caller then frees the workspace. */

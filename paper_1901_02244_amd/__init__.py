@@ -27,7 +27,7 @@ KIND_NAMES = {0: "conv_w", 1: "bias", 2: "bn_gamma", 3: "bn_beta", 4: "fc_w"}
 
 # The interface version these bindings are written for (CB_ABI_VERSION in
 # include/crossbow_sma.h); a library built from other sources is refused.
-ABI_VERSION = 3
+ABI_VERSION = 4
 
 # every symbol the header declares
 EXPORTS = (
@@ -42,6 +42,10 @@ EXPORTS = (
     "cb_test_conv_dgrad_parts", "cb_test_conv_dgrad", "cb_set_graphs", "cb_test_conv_by_pointer",
     "cb_test_conv_pointers", "cb_test_conv_dgrad_pointers", "cb_test_conv_kernel",
     "cb_test_bn_fwd_two", "cb_test_bn_bwd_two",
+    "cb_vocab_xent_workspace_bytes", "cb_vocab_xent_fwd", "cb_vocab_xent_bwd",
+    "cb_gated_norm_workspace_bytes", "cb_gated_norm_fwd", "cb_gated_norm_bwd",
+    "cb_ckpt_bytes", "cb_ckpt_pack", "cb_ckpt_unpack", "cb_ckpt_wgrad_workspace_bytes",
+    "cb_ckpt_wgrad",
 )
 
 
@@ -55,6 +59,22 @@ class cb_model(ctypes.Structure):
     _fields_ = [("arch", ctypes.c_int32), ("in_c", ctypes.c_int32), ("in_h", ctypes.c_int32),
                 ("in_w", ctypes.c_int32), ("num_classes", ctypes.c_int32),
                 ("learner_momentum", ctypes.c_float), ("check_finite", ctypes.c_int32)]
+
+
+class cb_vocab_xent(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("k", ctypes.c_int32), ("n", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("v", ctypes.c_int32), ("ignore", ctypes.c_int32),
+                ("h", ctypes.c_void_p), ("ldh", ctypes.c_int64), ("w", ctypes.c_void_p),
+                ("pstride", ctypes.c_int64), ("labels", ctypes.c_void_p)]
+
+
+class cb_gated_norm(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("k", ctypes.c_int32), ("n", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("gate_rows", ctypes.c_int32),
+                ("res_scale", ctypes.c_float), ("eps", ctypes.c_float),
+                ("block", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("post", ctypes.c_void_p),
+                ("pre", ctypes.c_void_p), ("post_stride", ctypes.c_int64),
+                ("pre_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -148,6 +168,22 @@ def lib():
         L.cb_learners.argtypes = [_P]
         L.cb_set_graphs.argtypes = [_P, _i]
         L.cb_tuner_next.argtypes = [_i, ctypes.c_double, ctypes.c_double, ctypes.c_double, _i]
+        _z, _q = ctypes.c_size_t, ctypes.c_int64
+        L.cb_vocab_xent_workspace_bytes.restype = _z
+        L.cb_vocab_xent_workspace_bytes.argtypes = [_P, _i]
+        L.cb_vocab_xent_fwd.argtypes = [_P] * 4 + [_z, _P]
+        L.cb_vocab_xent_bwd.argtypes = [_P, _P, ctypes.c_float, _P, _P, _q, _P, _z, _P]
+        L.cb_gated_norm_workspace_bytes.restype = _z
+        L.cb_gated_norm_workspace_bytes.argtypes = [_P]
+        L.cb_gated_norm_fwd.argtypes = [_P] * 6
+        L.cb_gated_norm_bwd.argtypes = [_P] * 8 + [_q, _P, _q, _P, _z, _P]
+        L.cb_ckpt_bytes.restype = _z
+        L.cb_ckpt_bytes.argtypes = [_q, _i]
+        L.cb_ckpt_pack.argtypes = [_i, _q, _i, _P, _P, _P]
+        L.cb_ckpt_unpack.argtypes = [_i, _q, _i, _P, _P, _P]
+        L.cb_ckpt_wgrad_workspace_bytes.restype = _z
+        L.cb_ckpt_wgrad_workspace_bytes.argtypes = [_i] * 5
+        L.cb_ckpt_wgrad.argtypes = [_i] * 5 + [_P, _P, _P, _q, _P, _z, _P]
         _lib = L
     return _lib
 
@@ -331,3 +367,339 @@ class Context:
         assert W.size == self.k * self.P and z.size == self.P and zprev.size == self.P
         return self._check(lib().cb_set_state(self._c, W.ctypes.data, z.ctypes.data,
                                               zprev.ctypes.data), "cb_set_state")
+
+
+# --- operators for language-model learners -------------------------------------
+# Tensors of k learners: activations [k, n, width], parameters and gradients with
+# the learner as their first dimension, which may be strided (a slice of a flat
+# [k, P] vector).  Outputs are allocated on the inputs' device; the work goes to
+# `stream`, or to torch's current stream of that device.  A workspace is a uint8
+# tensor that the caller keeps; without one each call takes its own from torch's
+# allocator.
+
+def _refuse(who, why):
+    raise CBError(CB_EINVAL, f"{who}: {why}")
+
+
+def _type_code(who, dtype):
+    import torch
+
+    code = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}.get(dtype)
+    if code is None:
+        _refuse(who, f"{dtype} is none of float32, float16, bfloat16")
+    return code
+
+
+def _need(who, name, t, shape, dtype, device, outer=False):
+    """Checks one tensor: its shape, type, device, and that it is contiguous (with
+    `outer`: apart from the stride of its first dimension)."""
+    if tuple(t.shape) != tuple(shape):
+        _refuse(who, f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
+    if t.dtype != dtype:
+        _refuse(who, f"{name} is {t.dtype}, not {dtype}")
+    if t.device != device or not t.is_cuda:
+        _refuse(who, f"{name} is on {t.device}, not on {device}, or not on a GPU")
+    if t.is_contiguous():
+        return
+    if not outer or t.dim() < 2 or t.numel() == 0 or not t[0].is_contiguous():
+        _refuse(who, f"{name} is not contiguous" + (" within a learner" if outer else ""))
+
+
+def _outer(t):
+    """Elements from one learner to the next."""
+    return t.stride(0) if t.shape[0] > 1 else t.numel()
+
+
+class _Call:
+    """The device and stream of one call: the device is current inside `with`, and
+    tensors that are handed to another stream than the one they came from are
+    known there to the allocator."""
+
+    def __init__(self, device, stream):
+        import torch
+
+        self.guard = torch.cuda.device(device)
+        self.device, self.given = device, stream
+
+    def __enter__(self):
+        import torch
+
+        self.guard.__enter__()
+        here = torch.cuda.current_stream()
+        self.stream = self.given if self.given is not None else here
+        self.other = self.stream != here
+        return self
+
+    def __exit__(self, *a):
+        return self.guard.__exit__(*a)
+
+    def new(self, shape, dtype):
+        import torch
+
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        if self.other:
+            t.record_stream(self.stream)
+        return t
+
+    def workspace(self, who, nbytes, given):
+        import torch
+
+        if given is None:
+            return self.new((max(nbytes, 1),), torch.uint8)
+        if given.dtype != torch.uint8 or not given.is_contiguous() or given.device != self.device:
+            _refuse(who, "the workspace is not a contiguous uint8 tensor on the inputs' device")
+        return given
+
+    def check(self, who, rc):
+        if rc:
+            raise CBError(rc, lib().cb_last_error(None).decode() or who)
+
+    @property
+    def handle(self):
+        return self.stream.cuda_stream
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _xent(who, h, w, labels, ignore):
+    import torch
+
+    code = _type_code(who, h.dtype)
+    if h.dim() != 3 or w.dim() != 3:
+        _refuse(who, "h is [k, n, d] and w [k, v, d]")
+    k, n, d = h.shape
+    v = w.shape[1]
+    if not h.is_cuda:
+        _refuse(who, "h is not on a GPU")
+    if min(k, n, d, v) < 1:
+        _refuse(who, "an empty dimension")
+    # rows of h may lie further apart than d, the same for all learners
+    ldh = h.stride(1) if n > 1 else h.stride(0) if k > 1 else d
+    if (d > 1 and h.stride(2) != 1) or ldh < d or (k > 1 and h.stride(0) != n * ldh):
+        _refuse(who, "h is not rows at one stride")
+    _need(who, "w", w, (k, v, d), h.dtype, h.device, outer=True)
+    _need(who, "labels", labels, (k, n), torch.int32, h.device)
+    return cb_vocab_xent(code, k, n, d, v, ignore, h.data_ptr(), ldh, w.data_ptr(), _outer(w),
+                         labels.data_ptr())
+
+
+def cb_vocab_xent_fwd(h, w, labels, ignore=-100, workspace=None, stream=None):
+    """Softmax cross-entropy of the logits h W^T over a large vocabulary, without
+    storing them.  h [k, n, d] and w [k, v, d] of one type (float32, float16,
+    bfloat16), labels int32 [k, n]; rows labelled `ignore` do not count.
+
+    Returns (loss [k], lse [k, n]) in float32: each learner's mean over its counted
+    rows (0 if none counts) and the rows' log-sum-exp, which the backward takes."""
+    import torch
+
+    who = "cb_vocab_xent_fwd"
+    x = _xent(who, h, w, labels, ignore)
+    with _Call(h.device, stream) as c:
+        loss, lse = c.new((x.k,), torch.float32), c.new((x.k, x.n), torch.float32)
+        nbytes = lib().cb_vocab_xent_workspace_bytes(ctypes.byref(x), 0)
+        ws = c.workspace(who, nbytes, workspace)
+        c.check(who, lib().cb_vocab_xent_fwd(ctypes.byref(x), loss.data_ptr(), lse.data_ptr(),
+                                             ws.data_ptr(), ws.numel(), c.handle))
+    return loss, lse
+
+
+def cb_vocab_xent_bwd(h, w, labels, lse, grad_scale=1.0, ignore=-100, dw=None, workspace=None,
+                      stream=None):
+    """The gradients of grad_scale * loss of cb_vocab_xent_fwd, given its lse:
+    (dh [k, n, d], dw [k, v, d]) in the inputs' type.  dw may be given, for
+    instance as a view of a flat gradient vector; it is overwritten."""
+    import torch
+
+    who = "cb_vocab_xent_bwd"
+    x = _xent(who, h, w, labels, ignore)
+    _need(who, "lse", lse, (x.k, x.n), torch.float32, h.device)
+    with _Call(h.device, stream) as c:
+        dh = c.new((x.k, x.n, x.d), h.dtype)
+        if dw is None:
+            dw = c.new((x.k, x.v, x.d), h.dtype)
+        else:
+            _need(who, "dw", dw, (x.k, x.v, x.d), h.dtype, h.device, outer=True)
+        nbytes = lib().cb_vocab_xent_workspace_bytes(ctypes.byref(x), 1)
+        ws = c.workspace(who, nbytes, workspace)
+        c.check(who, lib().cb_vocab_xent_bwd(ctypes.byref(x), lse.data_ptr(), grad_scale,
+                                             dh.data_ptr(), dw.data_ptr(), _outer(dw),
+                                             ws.data_ptr(), ws.numel(), c.handle))
+    return dh, dw
+
+
+def _norm(who, x, block, gate, gate_rows, res_scale, post, pre, eps):
+    import torch
+
+    code = _type_code(who, x.dtype)
+    if x.dim() != 3 or min(x.shape) < 1:
+        _refuse(who, "x is [k, n, d], none of them 0")
+    k, n, d = x.shape
+    if not x.is_cuda:
+        _refuse(who, "x is not on a GPU")
+    _need(who, "x", x, x.shape, x.dtype, x.device)
+    if block is not None:
+        _need(who, "block", block, x.shape, x.dtype, x.device)
+    if gate is not None:
+        if not 1 <= gate_rows < 2**31:
+            _refuse(who, "gate_rows is out of range")
+        _need(who, "gate", gate, (k, -(-n // gate_rows), d), x.dtype, x.device)
+    for name, t in (("post", post), ("pre", pre)):
+        if t is not None:
+            _need(who, name, t, (k, d), torch.float32, x.device, outer=True)
+    return cb_gated_norm(code, k, n, d, gate_rows if gate is not None else 1, res_scale, eps,
+                         _ptr(block), _ptr(gate), _ptr(post), _ptr(pre),
+                         _outer(post) if post is not None else 0,
+                         _outer(pre) if pre is not None else 0)
+
+
+def cb_gated_norm_fwd(x, block=None, gate=None, gate_rows=1, res_scale=1.0, post=None, pre=None,
+                      eps=1e-5, keep=False, stream=None):
+    """The norm after a block, its gate and residual scale, the addition to the
+    residual stream, and the norm before the next block, in one pass:
+
+        x_out = x + res_scale * gate * (post * rms(block));  y = pre * rms(x_out)
+
+    x, block [k, n, d] and gate [k, ceil(n/gate_rows), d] of one type, post and pre
+    float32 [k, d]; each of block, gate, post and pre may be None.
+
+    Returns (x_out, y), x_out being x without a block and y None without pre; with
+    keep also y in 8 bits, as cb_ckpt_pack gives it."""
+    who = "cb_gated_norm_fwd"
+    g = _norm(who, x, block, gate, gate_rows, res_scale, post, pre, eps)
+    if keep and pre is None:
+        _refuse(who, "keep without pre")
+    with _Call(x.device, stream) as c:
+        xo = c.new(x.shape, x.dtype) if block is not None else x
+        y = c.new(x.shape, x.dtype) if pre is not None else None
+        kept = _new_kept(c, x) if keep else None
+        c.check(who, lib().cb_gated_norm_fwd(ctypes.byref(g), x.data_ptr(), xo.data_ptr(), _ptr(y),
+                                             _ptr(kept.data) if keep else None, c.handle))
+    return (xo, y, kept) if keep else (xo, y)
+
+
+def cb_gated_norm_bwd(x_out, dy=None, dres=None, block=None, gate=None, gate_rows=1, res_scale=1.0,
+                      post=None, pre=None, eps=1e-5, dpost=None, dpre=None, workspace=None,
+                      stream=None):
+    """Backward of cb_gated_norm_fwd, given its x_out, the gradient dy at y (with
+    pre) and the gradient dres that reaches x_out along the stream (or None).
+
+    Returns a dict: dx, and where their parts are there dblock, dgate (summed over
+    the rows that share a gate row), dpost, dpre (float32 [k, d]; may be given as
+    views of a flat gradient vector, and are overwritten)."""
+    import torch
+
+    who = "cb_gated_norm_bwd"
+    g = _norm(who, x_out, block, gate, gate_rows, res_scale, post, pre, eps)
+    if (dy is None) != (pre is None):
+        _refuse(who, "dy goes with pre")
+    for name, t in (("dy", dy), ("dres", dres)):
+        if t is not None:
+            _need(who, name, t, x_out.shape, x_out.dtype, x_out.device)
+    for name, t, of in (("dpost", dpost, post), ("dpre", dpre, pre)):
+        if t is not None:
+            if of is None:
+                _refuse(who, f"{name} without its gamma")
+            _need(who, name, t, (g.k, g.d), torch.float32, x_out.device, outer=True)
+    with _Call(x_out.device, stream) as c:
+        out = {"dx": c.new(x_out.shape, x_out.dtype)}
+        if block is not None:
+            out["dblock"] = c.new(x_out.shape, x_out.dtype)
+        if gate is not None:
+            out["dgate"] = c.new(gate.shape, gate.dtype)
+        if post is not None:
+            out["dpost"] = dpost if dpost is not None else c.new((g.k, g.d), torch.float32)
+        if pre is not None:
+            out["dpre"] = dpre if dpre is not None else c.new((g.k, g.d), torch.float32)
+        ws = c.workspace(who, lib().cb_gated_norm_workspace_bytes(ctypes.byref(g)), workspace)
+        c.check(who, lib().cb_gated_norm_bwd(
+            ctypes.byref(g), x_out.data_ptr(), _ptr(dy), _ptr(dres), out["dx"].data_ptr(),
+            _ptr(out.get("dblock")), _ptr(out.get("dgate")), _ptr(out.get("dpost")),
+            _outer(out["dpost"]) if post is not None else 0, _ptr(out.get("dpre")),
+            _outer(out["dpre"]) if pre is not None else 0, ws.data_ptr(), ws.numel(), c.handle))
+    return out
+
+
+class Kept:
+    """Activations [k, n, d] of `dtype` in 8 bits: `data` is the library's buffer."""
+
+    __slots__ = ("data", "shape", "dtype")
+
+    def __init__(self, data, shape, dtype):
+        self.data, self.shape, self.dtype = data, tuple(shape), dtype
+
+
+def _new_kept(c, x):
+    import torch
+
+    k, n, d = x.shape
+    nbytes = lib().cb_ckpt_bytes(k * n, d)
+    if nbytes == 0:
+        _refuse("cb_ckpt_bytes", f"{tuple(x.shape)} is out of range")
+    return Kept(c.new((nbytes,), torch.uint8), x.shape, x.dtype)
+
+
+def _check_kept(who, kept):
+    """The type code of a Kept whose buffer is as long as its shape says."""
+    import torch
+
+    code = _type_code(who, kept.dtype)
+    need = lib().cb_ckpt_bytes(kept.shape[0] * kept.shape[1], kept.shape[2])
+    b = kept.data
+    if not b.is_cuda or b.dtype != torch.uint8 or not b.is_contiguous() or need == 0 \
+            or b.numel() < need:
+        _refuse(who, f"the kept buffer is not {need} bytes on a GPU")
+    return code
+
+
+def cb_ckpt_pack(x, stream=None):
+    """x [k, n, d] (float32, float16, bfloat16) in 8 bits a value and a power of two
+    for every 32 columns.  Returns a Kept."""
+    who = "cb_ckpt_pack"
+    code = _type_code(who, x.dtype)
+    if x.dim() != 3 or min(x.shape) < 1:
+        _refuse(who, "x is [k, n, d], none of them 0")
+    if not x.is_cuda:
+        _refuse(who, "x is not on a GPU")
+    _need(who, "x", x, x.shape, x.dtype, x.device)
+    with _Call(x.device, stream) as c:
+        kept = _new_kept(c, x)
+        c.check(who, lib().cb_ckpt_pack(code, x.shape[0] * x.shape[1], x.shape[2], x.data_ptr(),
+                                        kept.data.data_ptr(), c.handle))
+    return kept
+
+
+def cb_ckpt_unpack(kept, stream=None):
+    """The values that `kept` stands for, [k, n, d] in its type."""
+    who = "cb_ckpt_unpack"
+    code = _check_kept(who, kept)
+    k, n, d = kept.shape
+    with _Call(kept.data.device, stream) as c:
+        x = c.new(kept.shape, kept.dtype)
+        c.check(who, lib().cb_ckpt_unpack(code, k * n, d, kept.data.data_ptr(), x.data_ptr(),
+                                          c.handle))
+    return x
+
+
+def cb_ckpt_wgrad(kept, dy, dw=None, workspace=None, stream=None):
+    """The weight gradient of a linear layer whose input [k, n, d] was kept in 8
+    bits: dw [k, out, d] = dy^T x for dy [k, n, out] of the same type.  dw may be
+    given, for instance as a view of a flat gradient vector; it is overwritten."""
+    who = "cb_ckpt_wgrad"
+    code = _check_kept(who, kept)
+    k, n, d = kept.shape
+    if dy.dim() != 3 or dy.shape[2] < 1:
+        _refuse(who, "dy is [k, n, out]")
+    out = dy.shape[2]
+    _need(who, "dy", dy, (k, n, out), kept.dtype, kept.data.device)
+    with _Call(dy.device, stream) as c:
+        if dw is None:
+            dw = c.new((k, out, d), kept.dtype)
+        else:
+            _need(who, "dw", dw, (k, out, d), kept.dtype, dy.device, outer=True)
+        ws = c.workspace(who, lib().cb_ckpt_wgrad_workspace_bytes(code, k, n, d, out), workspace)
+        c.check(who, lib().cb_ckpt_wgrad(code, k, n, d, out, kept.data.data_ptr(), dy.data_ptr(),
+                                         dw.data_ptr(), _outer(dw), ws.data_ptr(), ws.numel(),
+                                         c.handle))
+    return dw

@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libcrossbow_sma.so")
 SOURCES = ["api.hip", "conv_gemm.hip", "conv_direct.hip", "layers.hip", "sma.hip", "test_hooks.hip",
-           "conv_static.hip", "lenet.hip"]
+           "conv_static.hip", "lenet.hip", "lm_api.hip", "vocab_xent.hip", "gated_norm.hip",
+           "ckpt.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

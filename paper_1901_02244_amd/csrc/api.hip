@@ -569,7 +569,7 @@ struct cb_ctx {
 
 namespace {
 
-std::string g_create_error;
+thread_local std::string g_create_error;
 
 }  // namespace
 

@@ -1,0 +1,174 @@
+"""What the language-model operators refuse, on the host: every check is made
+before any device is touched, so these run without a GPU, on addresses that
+are never followed."""
+import ctypes
+
+import pytest
+
+import paper_1901_02244_amd as cb
+
+torch = pytest.importorskip("torch")
+
+A = 1 << 40  # an aligned address
+BIG = 1 << 44
+
+
+def _err():
+    return cb.lib().cb_last_error(None).decode()
+
+
+def xent(**kw):
+    f = dict(type=2, k=2, n=16, d=64, v=1000, ignore=-100, h=A, ldh=64, w=A, pstride=64000, labels=A)
+    f.update(kw)
+    return cb.cb_vocab_xent(*(f[name] for name, _ in cb.cb_vocab_xent._fields_))
+
+
+XENT_WRONG = [dict(type=3), dict(type=-1), dict(k=0), dict(n=0), dict(d=0), dict(v=0), dict(k=70000),
+              dict(n=1 << 30, k=2), dict(d=(1 << 20) + 1), dict(h=None), dict(w=None), dict(labels=None),
+              dict(h=A + 1), dict(w=A + 1), dict(labels=A + 2), dict(ldh=63), dict(pstride=63999),
+              dict(k=-1), dict(n=-5), dict(v=1 << 30, n=1 << 20)]
+
+
+@pytest.mark.parametrize("kw", XENT_WRONG, ids=str)
+def test_xent_refuses(kw):
+    L, x = cb.lib(), xent(**kw)
+    assert L.cb_vocab_xent_workspace_bytes(ctypes.byref(x), 0) == 0
+    assert L.cb_vocab_xent_workspace_bytes(ctypes.byref(x), 1) == 0
+    assert L.cb_vocab_xent_fwd(ctypes.byref(x), A, A, A, BIG, None) == cb.CB_EINVAL
+    assert _err().startswith("cb_vocab_xent_fwd: ")
+    assert L.cb_vocab_xent_bwd(ctypes.byref(x), A, 1.0, A, A, 64000, A, BIG, None) == cb.CB_EINVAL
+    assert _err().startswith("cb_vocab_xent_bwd: ")
+
+
+def test_xent_refuses_outputs():
+    L, x = cb.lib(), xent()
+    r = ctypes.byref(x)
+    need = [L.cb_vocab_xent_workspace_bytes(r, b) for b in (0, 1)]
+    assert min(need) > 0
+    E, M = cb.CB_EINVAL, cb.CB_ENOMEM
+    fwd, bwd = L.cb_vocab_xent_fwd, L.cb_vocab_xent_bwd
+    assert fwd(None, A, A, A, BIG, None) == E and L.cb_vocab_xent_workspace_bytes(None, 0) == 0
+    assert fwd(r, None, A, A, BIG, None) == E and fwd(r, A, None, A, BIG, None) == E
+    assert fwd(r, A, A, None, BIG, None) == E and fwd(r, A, A, A + 128, BIG, None) == E
+    assert fwd(r, A, A, A, need[0] - 1, None) == M and "workspace" in _err()
+    assert bwd(r, A, 1.0, A, A, 64000, A, need[1] - 1, None) == M
+    assert bwd(r, None, 1.0, A, A, 64000, A, BIG, None) == E
+    assert bwd(r, A, float("nan"), A, A, 64000, A, BIG, None) == E
+    assert bwd(r, A, 1.0, None, A, 64000, A, BIG, None) == E
+    assert bwd(r, A, 1.0, A, None, 64000, A, BIG, None) == E
+    assert bwd(r, A, 1.0, A, A + 1, 64000, A, BIG, None) == E
+    assert bwd(r, A, 1.0, A, A, 63999, A, BIG, None) == E
+    assert bwd(r, A, 1.0, A, A, 64000, A + 8, BIG, None) == E
+
+
+def test_xent_workspace_holds_no_logits():
+    """128,000 words: the backward's workspace stays at its piece, whatever the vocabulary; a copy of
+    W only where its rows do not start on 16 bytes."""
+    L = cb.lib()
+    one = lambda **kw: L.cb_vocab_xent_workspace_bytes(ctypes.byref(xent(k=1, n=8192, d=4096, ldh=4096, **kw)), 1)
+    piece = 1 << 28
+    assert one(v=128000) < piece + 3 * 8192 * 4096 * 4
+    assert one(v=128000) == one(v=64000)
+    assert one(v=128000, w=A + 2) > one(v=128000) + 128000 * 4096 * 2 - 1
+
+
+def norm(**kw):
+    f = dict(type=2, k=2, n=16, d=64, gate_rows=4, res_scale=1.0, eps=1e-5, block=A, gate=A, post=A, pre=A,
+             post_stride=64, pre_stride=64)
+    f.update(kw)
+    return cb.cb_gated_norm(*(f[name] for name, _ in cb.cb_gated_norm._fields_))
+
+
+NORM_WRONG = [dict(type=3), dict(k=0), dict(n=0), dict(d=0), dict(d=16385), dict(n=1 << 30),
+              dict(res_scale=float("inf")), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")),
+              dict(block=None), dict(block=None, gate=None), dict(block=None, post=None),
+              dict(block=None, gate=None, post=None, pre=None), dict(gate_rows=0), dict(gate_rows=-1),
+              dict(block=A + 1), dict(gate=A + 1), dict(post=A + 2), dict(pre=A + 2), dict(post_stride=63),
+              dict(pre_stride=63)]
+
+
+@pytest.mark.parametrize("kw", NORM_WRONG, ids=str)
+def test_norm_refuses(kw):
+    L, g = cb.lib(), norm(**kw)
+    assert L.cb_gated_norm_workspace_bytes(ctypes.byref(g)) == 0
+    assert L.cb_gated_norm_fwd(ctypes.byref(g), A, A, A, None, None) == cb.CB_EINVAL
+    assert L.cb_gated_norm_bwd(ctypes.byref(g), A, A, A, A, A, A, A, 64, A, 64, A, BIG, None) == cb.CB_EINVAL
+    assert _err().startswith("cb_gated_norm_bwd: ")
+
+
+def test_norm_refuses_tensors():
+    L, E = cb.lib(), cb.CB_EINVAL
+    g = norm()
+    r = ctypes.byref(g)
+    need = L.cb_gated_norm_workspace_bytes(r)
+    assert need > 0
+    fwd = L.cb_gated_norm_fwd
+    assert fwd(r, None, A, A, None, None) == E and fwd(r, A, None, A, None, None) == E
+    assert fwd(r, A, A, None, None, None) == E and fwd(r, A, A, A, A + 8, None) == E
+    no_pre = norm(pre=None)
+    assert fwd(ctypes.byref(no_pre), A, A, None, A, None) == E  # 8 bits of nothing
+    args = [A, A, A, A, A, A, A, 64, A, 64, A, need, None]
+
+    def bwd(d, at, v):
+        a = list(args)
+        a[at] = v
+        return L.cb_gated_norm_bwd(ctypes.byref(d), *a)
+
+    for at in (0, 1, 3, 4, 5, 6, 8, 10):  # every buffer but dres is needed here
+        assert bwd(g, at, None) == E, at
+    for at in (0, 1, 2, 3, 4, 5, 6, 8, 10):
+        assert bwd(g, at, A + 1) == E, at
+    assert bwd(g, 7, 63) == E and bwd(g, 9, 63) == E
+    assert bwd(g, 11, need - 1) == cb.CB_ENOMEM
+    assert bwd(no_pre, 2, A) == E  # dy without pre
+    a = list(args)
+    a[1] = a[2] = None
+    assert L.cb_gated_norm_bwd(ctypes.byref(no_pre), *a) == E  # no gradient comes in
+
+
+def test_ckpt_refuses():
+    L, E = cb.lib(), cb.CB_EINVAL
+    assert L.cb_ckpt_bytes(0, 32) == 0 and L.cb_ckpt_bytes(4, 0) == 0 and L.cb_ckpt_bytes(1, 1 << 21) == 0
+    assert L.cb_ckpt_bytes((1 << 30) + 1, 1) == 0
+    assert L.cb_ckpt_bytes(3, 33) >= 3 * 66
+    for f in (L.cb_ckpt_pack, L.cb_ckpt_unpack):
+        assert f(3, 4, 32, A, A, None) == E and f(0, 0, 32, A, A, None) == E and f(0, 4, 0, A, A, None) == E
+        assert f(0, 4, 32, None, A, None) == E and f(0, 4, 32, A, None, None) == E
+    assert L.cb_ckpt_pack(2, 4, 32, A + 1, A, None) == E and L.cb_ckpt_pack(2, 4, 32, A, A + 8, None) == E
+    assert L.cb_ckpt_unpack(2, 4, 32, A + 8, A, None) == E and L.cb_ckpt_unpack(2, 4, 32, A, A + 1, None) == E
+    size, w = L.cb_ckpt_wgrad_workspace_bytes, L.cb_ckpt_wgrad
+    need = size(2, 2, 16, 64, 32)
+    assert need > 0
+    for bad in ((3, 2, 16, 64, 32), (2, 0, 16, 64, 32), (2, 2, 0, 64, 32), (2, 2, 16, 0, 32), (2, 2, 16, 64, 0),
+                (2, 2, 16, (1 << 20) + 1, 32), (2, 2, 16, 64, (1 << 20) + 1), (2, 2, 1 << 30, 64, 32)):
+        assert size(*bad) == 0
+        assert w(*bad, A, A, A, 1 << 30, A, BIG, None) == E
+    ok = (2, 2, 16, 64, 32)
+    assert w(*ok, None, A, A, 2048, A, BIG, None) == E and w(*ok, A, None, A, 2048, A, BIG, None) == E
+    assert w(*ok, A, A, None, 2048, A, BIG, None) == E and w(*ok, A, A, A, 2047, A, BIG, None) == E
+    assert w(*ok, A, A, A, 2048, A + 64, BIG, None) == E
+    assert w(*ok, A, A, A, 2048, A, need - 1, None) == cb.CB_ENOMEM
+
+
+def test_package_refuses_cpu_and_misshapen_tensors():
+    """The package checks shapes, types and places before it calls the library."""
+    z = torch.zeros
+    i = z(1, 4, dtype=torch.int32)
+    bad = [
+        lambda: cb.cb_vocab_xent_fwd(z(1, 4, 8), z(1, 9, 8), i),  # not on a GPU
+        lambda: cb.cb_vocab_xent_fwd(z(1, 4, 8, dtype=torch.float64), z(1, 9, 8), i),
+        lambda: cb.cb_vocab_xent_fwd(z(4, 8), z(9, 8), i),
+        lambda: cb.cb_vocab_xent_bwd(z(1, 4, 8), z(1, 9, 8), i, z(1, 4)),
+        lambda: cb.cb_gated_norm_fwd(z(1, 4, 8), pre=z(1, 8)),
+        lambda: cb.cb_gated_norm_fwd(z(4, 8), pre=z(1, 8)),
+        lambda: cb.cb_gated_norm_fwd(z(1, 0, 8), pre=z(1, 8)),
+        lambda: cb.cb_gated_norm_bwd(z(1, 4, 8), dy=z(1, 4, 8), pre=z(1, 8)),
+        lambda: cb.cb_ckpt_pack(z(1, 4, 8)),
+        lambda: cb.cb_ckpt_pack(z(1, 4, 8, dtype=torch.int32)),
+        lambda: cb.cb_ckpt_wgrad(cb.Kept(z(64, dtype=torch.uint8), (1, 4, 8), torch.float32), z(1, 4, 3)),
+        lambda: cb.cb_ckpt_unpack(cb.Kept(z(64, dtype=torch.uint8), (1, 4, 8), torch.float32)),
+    ]
+    for f in bad:
+        with pytest.raises(cb.CBError) as e:
+            f()
+        assert e.value.code == cb.CB_EINVAL
