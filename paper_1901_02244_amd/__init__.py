@@ -79,6 +79,7 @@ class cb_gated_norm(ctypes.Structure):
 
 _lib = None
 _P = ctypes.c_void_p
+_ref = ctypes.byref
 
 
 def check_abi(L, path):
@@ -381,27 +382,35 @@ def _refuse(who, why):
     raise CBError(CB_EINVAL, f"{who}: {why}")
 
 
-def _type_code(who, dtype):
-    import torch
+_type_codes = {}
 
-    code = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}.get(dtype)
+
+def _type_code(who, dtype):
+    code = _type_codes.get(dtype)
     if code is None:
-        _refuse(who, f"{dtype} is none of float32, float16, bfloat16")
+        import torch
+
+        _type_codes.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+        code = _type_codes.get(dtype)
+        if code is None:
+            _refuse(who, f"{dtype} is none of float32, float16, bfloat16")
     return code
 
 
 def _need(who, name, t, shape, dtype, device, outer=False):
     """Checks one tensor: its shape, type, device, and that it is contiguous (with
     `outer`: apart from the stride of its first dimension)."""
-    if tuple(t.shape) != tuple(shape):
+    if t.shape == shape and t.dtype is dtype and t.device == device and t.is_cuda \
+            and t.is_contiguous():
+        return
+    if t.shape != tuple(shape):
         _refuse(who, f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
     if t.dtype != dtype:
         _refuse(who, f"{name} is {t.dtype}, not {dtype}")
-    if t.device != device or not t.is_cuda:
+    if not t.is_cuda or t.device != device:
         _refuse(who, f"{name} is on {t.device}, not on {device}, or not on a GPU")
-    if t.is_contiguous():
-        return
-    if not outer or t.dim() < 2 or t.numel() == 0 or not t[0].is_contiguous():
+    if not t.is_contiguous() and not (outer and t.dim() > 1 and t.numel()
+                                      and t[0].is_contiguous()):
         _refuse(who, f"{name} is not contiguous" + (" within a learner" if outer else ""))
 
 
@@ -411,42 +420,51 @@ def _outer(t):
 
 
 class _Call:
-    """The device and stream of one call: the device is current inside `with`, and
-    tensors that are handed to another stream than the one they came from are
-    known there to the allocator."""
+    """The device and stream of one call: the device of `t` is current inside
+    `with`, and tensors that are made for another stream than torch's current one
+    are known there to the allocator."""
 
-    def __init__(self, device, stream):
+    __slots__ = ("torch", "device", "index", "back", "given", "handle", "other")
+
+    def __init__(self, t, stream):
         import torch
 
-        self.guard = torch.cuda.device(device)
-        self.device, self.given = device, stream
+        self.torch, self.device, self.index, self.given = torch, t.device, t.get_device(), stream
 
     def __enter__(self):
-        import torch
-
-        self.guard.__enter__()
-        here = torch.cuda.current_stream()
-        self.stream = self.given if self.given is not None else here
-        self.other = self.stream != here
+        cuda = self.torch.cuda
+        now = cuda.current_device()
+        self.back = now if now != self.index else -1
+        if self.back >= 0:
+            cuda.set_device(self.index)
+        self.handle = here = _current_stream(self.torch, self.index)
+        self.other = False
+        if self.given is not None:
+            self.handle = self.given.cuda_stream
+            self.other = self.handle != here
         return self
 
     def __exit__(self, *a):
-        return self.guard.__exit__(*a)
+        if self.back >= 0:
+            self.torch.cuda.set_device(self.back)
 
     def new(self, shape, dtype):
-        import torch
-
-        t = torch.empty(shape, dtype=dtype, device=self.device)
+        t = self.torch.empty(shape, dtype=dtype, device=self.device)
         if self.other:
-            t.record_stream(self.stream)
+            t.record_stream(self.given)
         return t
 
-    def workspace(self, who, nbytes, given):
-        import torch
+    def like(self, t):
+        n = self.torch.empty_like(t)
+        if self.other:
+            n.record_stream(self.given)
+        return n
 
+    def workspace(self, who, nbytes, given):
         if given is None:
-            return self.new((max(nbytes, 1),), torch.uint8)
-        if given.dtype != torch.uint8 or not given.is_contiguous() or given.device != self.device:
+            return self.new((max(nbytes, 1),), self.torch.uint8)
+        if given.dtype != self.torch.uint8 or not given.is_contiguous() \
+                or given.device != self.device:
             _refuse(who, "the workspace is not a contiguous uint8 tensor on the inputs' device")
         return given
 
@@ -454,9 +472,12 @@ class _Call:
         if rc:
             raise CBError(rc, lib().cb_last_error(None).decode() or who)
 
-    @property
-    def handle(self):
-        return self.stream.cuda_stream
+
+def _current_stream(torch, index):
+    """The handle of torch's current stream of a device (the stream object itself
+    takes microseconds to make)."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 def _ptr(t):
@@ -496,11 +517,11 @@ def cb_vocab_xent_fwd(h, w, labels, ignore=-100, workspace=None, stream=None):
 
     who = "cb_vocab_xent_fwd"
     x = _xent(who, h, w, labels, ignore)
-    with _Call(h.device, stream) as c:
+    with _Call(h, stream) as c:
         loss, lse = c.new((x.k,), torch.float32), c.new((x.k, x.n), torch.float32)
-        nbytes = lib().cb_vocab_xent_workspace_bytes(ctypes.byref(x), 0)
+        nbytes = lib().cb_vocab_xent_workspace_bytes(_ref(x), 0)
         ws = c.workspace(who, nbytes, workspace)
-        c.check(who, lib().cb_vocab_xent_fwd(ctypes.byref(x), loss.data_ptr(), lse.data_ptr(),
+        c.check(who, lib().cb_vocab_xent_fwd(_ref(x), loss.data_ptr(), lse.data_ptr(),
                                              ws.data_ptr(), ws.numel(), c.handle))
     return loss, lse
 
@@ -515,15 +536,15 @@ def cb_vocab_xent_bwd(h, w, labels, lse, grad_scale=1.0, ignore=-100, dw=None, w
     who = "cb_vocab_xent_bwd"
     x = _xent(who, h, w, labels, ignore)
     _need(who, "lse", lse, (x.k, x.n), torch.float32, h.device)
-    with _Call(h.device, stream) as c:
+    with _Call(h, stream) as c:
         dh = c.new((x.k, x.n, x.d), h.dtype)
         if dw is None:
             dw = c.new((x.k, x.v, x.d), h.dtype)
         else:
             _need(who, "dw", dw, (x.k, x.v, x.d), h.dtype, h.device, outer=True)
-        nbytes = lib().cb_vocab_xent_workspace_bytes(ctypes.byref(x), 1)
+        nbytes = lib().cb_vocab_xent_workspace_bytes(_ref(x), 1)
         ws = c.workspace(who, nbytes, workspace)
-        c.check(who, lib().cb_vocab_xent_bwd(ctypes.byref(x), lse.data_ptr(), grad_scale,
+        c.check(who, lib().cb_vocab_xent_bwd(_ref(x), lse.data_ptr(), grad_scale,
                                              dh.data_ptr(), dw.data_ptr(), _outer(dw),
                                              ws.data_ptr(), ws.numel(), c.handle))
     return dh, dw
@@ -570,11 +591,11 @@ def cb_gated_norm_fwd(x, block=None, gate=None, gate_rows=1, res_scale=1.0, post
     g = _norm(who, x, block, gate, gate_rows, res_scale, post, pre, eps)
     if keep and pre is None:
         _refuse(who, "keep without pre")
-    with _Call(x.device, stream) as c:
-        xo = c.new(x.shape, x.dtype) if block is not None else x
-        y = c.new(x.shape, x.dtype) if pre is not None else None
+    with _Call(x, stream) as c:
+        xo = c.like(x) if block is not None else x
+        y = c.like(x) if pre is not None else None
         kept = _new_kept(c, x) if keep else None
-        c.check(who, lib().cb_gated_norm_fwd(ctypes.byref(g), x.data_ptr(), xo.data_ptr(), _ptr(y),
+        c.check(who, lib().cb_gated_norm_fwd(_ref(g), x.data_ptr(), xo.data_ptr(), _ptr(y),
                                              _ptr(kept.data) if keep else None, c.handle))
     return (xo, y, kept) if keep else (xo, y)
 
@@ -602,19 +623,19 @@ def cb_gated_norm_bwd(x_out, dy=None, dres=None, block=None, gate=None, gate_row
             if of is None:
                 _refuse(who, f"{name} without its gamma")
             _need(who, name, t, (g.k, g.d), torch.float32, x_out.device, outer=True)
-    with _Call(x_out.device, stream) as c:
-        out = {"dx": c.new(x_out.shape, x_out.dtype)}
+    with _Call(x_out, stream) as c:
+        out = {"dx": c.like(x_out)}
         if block is not None:
-            out["dblock"] = c.new(x_out.shape, x_out.dtype)
+            out["dblock"] = c.like(x_out)
         if gate is not None:
-            out["dgate"] = c.new(gate.shape, gate.dtype)
+            out["dgate"] = c.like(gate)
         if post is not None:
             out["dpost"] = dpost if dpost is not None else c.new((g.k, g.d), torch.float32)
         if pre is not None:
             out["dpre"] = dpre if dpre is not None else c.new((g.k, g.d), torch.float32)
-        ws = c.workspace(who, lib().cb_gated_norm_workspace_bytes(ctypes.byref(g)), workspace)
+        ws = c.workspace(who, lib().cb_gated_norm_workspace_bytes(_ref(g)), workspace)
         c.check(who, lib().cb_gated_norm_bwd(
-            ctypes.byref(g), x_out.data_ptr(), _ptr(dy), _ptr(dres), out["dx"].data_ptr(),
+            _ref(g), x_out.data_ptr(), _ptr(dy), _ptr(dres), out["dx"].data_ptr(),
             _ptr(out.get("dblock")), _ptr(out.get("dgate")), _ptr(out.get("dpost")),
             _outer(out["dpost"]) if post is not None else 0, _ptr(out.get("dpre")),
             _outer(out["dpre"]) if pre is not None else 0, ws.data_ptr(), ws.numel(), c.handle))
@@ -663,7 +684,7 @@ def cb_ckpt_pack(x, stream=None):
     if not x.is_cuda:
         _refuse(who, "x is not on a GPU")
     _need(who, "x", x, x.shape, x.dtype, x.device)
-    with _Call(x.device, stream) as c:
+    with _Call(x, stream) as c:
         kept = _new_kept(c, x)
         c.check(who, lib().cb_ckpt_pack(code, x.shape[0] * x.shape[1], x.shape[2], x.data_ptr(),
                                         kept.data.data_ptr(), c.handle))
@@ -675,7 +696,7 @@ def cb_ckpt_unpack(kept, stream=None):
     who = "cb_ckpt_unpack"
     code = _check_kept(who, kept)
     k, n, d = kept.shape
-    with _Call(kept.data.device, stream) as c:
+    with _Call(kept.data, stream) as c:
         x = c.new(kept.shape, kept.dtype)
         c.check(who, lib().cb_ckpt_unpack(code, k * n, d, kept.data.data_ptr(), x.data_ptr(),
                                           c.handle))
@@ -693,7 +714,7 @@ def cb_ckpt_wgrad(kept, dy, dw=None, workspace=None, stream=None):
         _refuse(who, "dy is [k, n, out]")
     out = dy.shape[2]
     _need(who, "dy", dy, (k, n, out), kept.dtype, kept.data.device)
-    with _Call(dy.device, stream) as c:
+    with _Call(dy, stream) as c:
         if dw is None:
             dw = c.new((k, out, d), kept.dtype)
         else:

@@ -13,15 +13,15 @@ namespace cbk {
 namespace {
 
 // x [rows][d] to q and group bytes.
-template <class T>
-__global__ __launch_bounds__(256) void kept_pack_k(const T* x, int64_t rows, int d, bool vec,
-                                                   char* q, uint8_t* e) {
+template <class T, bool WHOLE>
+__global__ __launch_bounds__(256) void kept_pack_k(const T* x, int64_t rows, int d, char* q,
+                                                   uint8_t* e) {
   const int64_t dp = kept_dp(d), units = rows * (dp / 8);
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < units; i += gridDim.x * 256ll) {
     const int64_t r = i / (dp / 8);
     const int c = (int)(i - r * (dp / 8)) * 8;
     float v[8];
-    load8<T>(x + r * d, c, d, vec, v);
+    load8<T, WHOLE>(x + r * d, c, d, v);
     uint32_t most = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) most = max(most, abs_bits(v[k]));
@@ -34,9 +34,9 @@ __global__ __launch_bounds__(256) void kept_pack_k(const T* x, int64_t rows, int
 }
 
 // and back: [rows][d], or with ld > d rows that far apart, zeros between
-template <class T>
+template <class T, bool WHOLE>
 __global__ __launch_bounds__(256) void kept_unpack_k(const char* q, const uint8_t* e, int64_t rows,
-                                                     int d, bool vec, T* x, int64_t ld) {
+                                                     int d, T* x, int64_t ld) {
   const int64_t dp = kept_dp(d), units = rows * (dp / 8);
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < units; i += gridDim.x * 256ll) {
     const int64_t r = i / (dp / 8);
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void kept_unpack_k(const char* q, const uint8_
     float v[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = (float)(int8_t)(b >> (8 * k)) * s;
-    store8<T>(x + r * ld, c, ld > d ? (int)ld : d, vec, v);
+    store8<T, WHOLE>(x + r * ld, c, (int)ld, v);
   }
 }
 
@@ -168,27 +168,17 @@ unsigned blocks_of(int64_t units) { return (unsigned)std::min<int64_t>((units + 
 template <class T>
 hipError_t unpack(int64_t rows, int d, const void* kept, T* x, int64_t ld, hipStream_t s) {
   const int64_t dp = kept_dp(d);
-  const bool vec = ld % 8 == 0 && (uintptr_t)x % 16 == 0;
-  klaunch(kept_unpack_k<T>, dim3(blocks_of(rows * (dp / 8))), dim3(256), 0, s, (const char*)kept,
-          (const uint8_t*)kept + rows * dp, rows, d, vec, x, ld);
+  klaunch(ld % 8 ? kept_unpack_k<T, false> : kept_unpack_k<T, true>,
+          dim3(blocks_of(rows * (dp / 8))), dim3(256), 0, s, (const char*)kept,
+          (const uint8_t*)kept + rows * dp, rows, d, x, ld);
   return hipGetLastError();
 }
 
 template <class T>
 hipError_t pack(int64_t rows, int d, const void* x, void* kept, hipStream_t s) {
   const int64_t dp = kept_dp(d);
-  const bool vec = d % 8 == 0 && (uintptr_t)x % 16 == 0;
-  klaunch(kept_pack_k<T>, dim3(blocks_of(rows * (dp / 8))), dim3(256), 0, s, (const T*)x, rows, d,
-          vec, (char*)kept, (uint8_t*)kept + rows * dp);
-  return hipGetLastError();
-}
-
-template <class TL>
-hipError_t launch_grad(dim3 grid, const GradArgs& a, hipStream_t s) {
-  if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kept_grad_k<TL>),
-                                         hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS))
-    return e;
-  klaunch(kept_grad_k<TL>, grid, dim3(TL::THREADS), TL::LDS, s, a);
+  klaunch(d % 8 ? kept_pack_k<T, false> : kept_pack_k<T, true>, dim3(blocks_of(rows * (dp / 8))),
+          dim3(256), 0, s, (const T*)x, rows, d, (char*)kept, (uint8_t*)kept + rows * dp);
   return hipGetLastError();
 }
 
@@ -218,8 +208,9 @@ hipError_t grad(const KeptGradArgs& a, hipStream_t s) {
   g.vec = a.d % 4 == 0 && (uintptr_t)a.dw % (4 * sizeof(T)) == 0 && a.dstride % 4 == 0;
   g.part = l.splits > 1 ? (float*)(ws + l.part) : nullptr;
   const dim3 grid((unsigned)tiles(a.d, a.out, l.big ? 256 : 128), a.k, l.splits);
-  if (hipError_t e = l.big ? launch_grad<Big<T>>(grid, g, s) : launch_grad<Mid<T>>(grid, g, s))
-    return e;
+  hipError_t e = l.big ? launch_tile<Big<T>, kept_grad_k<Big<T>>>(grid, s, g)
+                       : launch_tile<Mid<T>, kept_grad_k<Mid<T>>>(grid, s, g);
+  if (e) return e;
   if (l.splits == 1) return hipSuccess;
   klaunch(kept_grad_join<T>, dim3(blocks_of((int64_t)a.out * a.d), a.k), dim3(256), 0, s,
           (const float*)g.part, l.splits, a.out, a.d, (T*)a.dw, a.dstride);

@@ -34,11 +34,28 @@ struct Split {
   __host__ __device__ int workers() const { return spans * per; }
 };
 
-// About 1024 workers in all: four workgroups for every CU where a worker is
-// one, with few enough rows of partial sums.
-Split split_rows(int k, int n, int gate_rows) {
-  const int target = std::max(1, 1024 / k);
-  const int each = std::max(1, (n + target - 1) / target);
+// The shape of a worker for rows of d: TPR threads of U * 8 columns.  Of the
+// 16-bit types a thread takes two eights from 512 columns on: the backward
+// kernel's registers allow two waves a SIMD either way, and twice as much is
+// in flight; of fp32, which would spill, only above 8192.
+struct Shape {
+  int tpr, u;
+};
+Shape shape_of(int type, int d) {
+  if (d <= 512) return {d <= 64 ? 8 : d <= 128 ? 16 : d <= 256 ? 32 : 64, 1};
+  const int eights = (d + 7) / 8;
+  for (int tpr = 64; tpr < 1024; tpr *= 2)
+    if (eights <= tpr * (type == LM_F32 ? 1 : 2)) return {tpr, type == LM_F32 ? 1 : 2};
+  return {1024, eights <= 1024 ? 1 : 2};
+}
+constexpr int threads_of(int tpr) { return tpr < 128 ? 256 : tpr; }
+
+// 512 threads for every CU, the two waves a SIMD that the backward kernel's
+// registers let be resident, and at least four rows a worker where the rows
+// are few, so that the partial sums stay a small part of what is read.
+Split split_rows(int type, int k, int n, int d, int gate_rows) {
+  const int target = std::max(1, 256 * 512 / shape_of(type, d).tpr / k);
+  const int each = std::max(std::min(n, 4), (n + target - 1) / target);
   Split s;
   if (gate_rows <= each) {
     s.span = (each + gate_rows - 1) / gate_rows * gate_rows;
@@ -55,7 +72,6 @@ Split split_rows(int k, int n, int gate_rows) {
 struct Dev {
   NormArgs a;
   Split s;
-  bool vec;
   float* part;    // [k][workers][3][d] partial sums of dpre, dpost, dgate
 };
 
@@ -72,11 +88,12 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[N]) {
 #pragma unroll
       for (int i = 0; i < N; ++i) lds[wave][i] = v[i];
     __syncthreads();
+    constexpr int W = TPR / 64;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      v[i] = 0.f;
+      v[i] = lds[threadIdx.x % W][i];
 #pragma unroll
-      for (int w = 0; w < TPR / 64; ++w) v[i] += lds[w][i];
+      for (int o = W / 2; o; o >>= 1) v[i] += __shfl_xor(v[i], o);
     }
   }
 }
@@ -84,10 +101,10 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[N]) {
 template <int U>
 using Row = float[U][8];
 
-template <int TPR, int U, class T>
-__device__ __forceinline__ void load_row(const T* row, int t, int d, bool vec, Row<U>& x) {
+template <int TPR, int U, bool WHOLE, class T>
+__device__ __forceinline__ void load_row(const T* row, int t, int d, Row<U>& x) {
 #pragma unroll
-  for (int u = 0; u < U; ++u) load8<T>(row, (u * TPR + t) * 8, d, vec, x[u]);
+  for (int u = 0; u < U; ++u) load8<T, WHOLE>(row, (u * TPR + t) * 8, d, x[u]);
 }
 template <int U>
 __device__ __forceinline__ void fill_row(Row<U>& x, float v) {
@@ -97,15 +114,29 @@ __device__ __forceinline__ void fill_row(Row<U>& x, float v) {
     for (int i = 0; i < 8; ++i) x[u][i] = v;
 }
 // gamma of this learner, or ones
-template <int TPR, int U>
+template <int TPR, int U, bool WHOLE>
 __device__ __forceinline__ void load_gamma(const float* g, int64_t stride, int j, int t, int d,
                                            Row<U>& x) {
   fill_row<U>(x, 1.f);
-  const float* row = g + j * stride;
-  if (g) load_row<TPR, U, float>(row, t, d, d % 8 == 0 && (uintptr_t)row % 16 == 0, x);
+  if (g) load_row<TPR, U, WHOLE, float>(g + j * stride, t, d, x);
 }
-
-constexpr int threads_of(int tpr) { return tpr < 256 ? 256 : tpr; }
+// A row as it lies in memory (zeros without one), to be converted where it is
+// used: half the registers, for 16-bit types, of the floats.
+template <class T, int U>
+struct RawRow {
+  Raw8<T> u[U];
+};
+template <int TPR, int U, bool WHOLE, class T>
+__device__ __forceinline__ void load_raw(const void* base, int64_t at, int t, int d,
+                                         RawRow<T, U>& x) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (base)
+      x.u[u] = load_raw8<T, WHOLE>((const T*)base + at, (u * TPR + t) * 8, d);
+    else
+      x.u[u] = Raw8<T>{};
+  }
+}
 
 // The rows of this worker: false if it has none.
 template <int TPR>
@@ -118,7 +149,7 @@ __device__ __forceinline__ bool my_rows(const Dev& v, int& worker, int& r0, int&
   return true;
 }
 
-template <class T, int TPR, int U>
+template <class T, int TPR, int U, bool WHOLE>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_forward(Dev v) {
   const NormArgs& a = v.a;
   const int j = blockIdx.y, t = threadIdx.x % TPR, d = a.d;
@@ -126,8 +157,8 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_forward(Dev v) {
   int worker, r0, r1;
   if (!my_rows<TPR>(v, worker, r0, r1)) return;
   Row<U> post, pre, gate;
-  load_gamma<TPR, U>(a.post, a.post_stride, j, t, d, post);
-  load_gamma<TPR, U>(a.pre, a.pre_stride, j, t, d, pre);
+  load_gamma<TPR, U, WHOLE>(a.post, a.post_stride, j, t, d, post);
+  load_gamma<TPR, U, WHOLE>(a.pre, a.pre_stride, j, t, d, pre);
   fill_row<U>(gate, 1.f);
   const int groups = (a.n + a.gate_rows - 1) / a.gate_rows;
   int group = -1;
@@ -135,13 +166,13 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_forward(Dev v) {
   for (int r = r0; r < r1; ++r) {
     const int64_t at = ((int64_t)j * a.n + r) * d;
     Row<U> x;
-    load_row<TPR, U>((const T*)a.x + at, t, d, v.vec, x);
+    load_row<TPR, U, WHOLE>((const T*)a.x + at, t, d, x);
     if (a.block) {
       Row<U> o;
-      load_row<TPR, U>((const T*)a.block + at, t, d, v.vec, o);
+      load_row<TPR, U, WHOLE>((const T*)a.block + at, t, d, o);
       if (a.gate && group != r / a.gate_rows) {
         group = r / a.gate_rows;
-        load_row<TPR, U>((const T*)a.gate + ((int64_t)j * groups + group) * d, t, d, v.vec, gate);
+        load_row<TPR, U, WHOLE>((const T*)a.gate + ((int64_t)j * groups + group) * d, t, d, gate);
       }
       float ro = 1.f;
       if (a.post) {
@@ -158,7 +189,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_forward(Dev v) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           x[u][i] += a.res_scale * gate[u][i] * (post[u][i] * (o[u][i] * ro));
-        store8<T>((T*)a.x_out + at, (u * TPR + t) * 8, d, v.vec, x[u]);
+        store8<T, WHOLE>((T*)a.x_out + at, (u * TPR + t) * 8, d, x[u]);
       }
     }
     if (!a.pre) continue;
@@ -174,7 +205,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_forward(Dev v) {
       const int c = (u * TPR + t) * 8;
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[u][i] = pre[u][i] * (x[u][i] * rx);
-      store8<T>((T*)a.y + at, c, d, v.vec, x[u]);
+      store8<T, WHOLE>((T*)a.y + at, c, d, x[u]);
       if (a.y_kept) {
         // the 8-bit form of y as stored: four lanes hold a group
         const int64_t dp = kept_dp(d), row = (int64_t)j * a.n + r;
@@ -197,16 +228,16 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_forward(Dev v) {
   }
 }
 
-template <class T, int TPR, int U>
-__global__ __launch_bounds__(threads_of(TPR)) void norm_backward(Dev v) {
+template <class T, int TPR, int U, bool WHOLE>
+__global__ __launch_bounds__(threads_of(TPR), TPR > 512 ? 4 : 2) void norm_backward(Dev v) {
   const NormArgs& a = v.a;
   const int j = blockIdx.y, t = threadIdx.x % TPR, d = a.d;
   __shared__ float lds_a[TPR / 64 + 1][3], lds_b[TPR / 64 + 1][1];
   int worker, r0, r1;
   if (!my_rows<TPR>(v, worker, r0, r1)) return;
   Row<U> post, pre, gate, dpre, dpost, dgate;
-  load_gamma<TPR, U>(a.post, a.post_stride, j, t, d, post);
-  load_gamma<TPR, U>(a.pre, a.pre_stride, j, t, d, pre);
+  load_gamma<TPR, U, WHOLE>(a.post, a.post_stride, j, t, d, post);
+  load_gamma<TPR, U, WHOLE>(a.pre, a.pre_stride, j, t, d, pre);
   fill_row<U>(gate, 1.f);
   fill_row<U>(dpre, 0.f);
   fill_row<U>(dpost, 0.f);
@@ -214,23 +245,35 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_backward(Dev v) {
   const int groups = (a.n + a.gate_rows - 1) / a.gate_rows;
   int group = -1;
   const float inv_d = 1.f / d;
+  // The next row's loads are in flight while a row is worked on.
+  struct Rows {
+    RawRow<T, U> x, dy, dres, o;
+  };
+  Rows next;
+  auto fetch = [&](int r) {
+    const int64_t at = ((int64_t)j * a.n + r) * d;
+    load_raw<TPR, U, WHOLE, T>(a.x, at, t, d, next.x);
+    load_raw<TPR, U, WHOLE, T>(a.dy, at, t, d, next.dy);
+    load_raw<TPR, U, WHOLE, T>(a.dres, at, t, d, next.dres);
+    load_raw<TPR, U, WHOLE, T>(a.block, at, t, d, next.o);
+  };
+  if (r0 < r1) fetch(r0);
   for (int r = r0; r < r1; ++r) {
     const int64_t at = ((int64_t)j * a.n + r) * d;
     Row<U> x, dy, dx, o;
-    fill_row<U>(dx, 0.f);
-    fill_row<U>(dy, 0.f);
-    fill_row<U>(o, 0.f);
-    if (a.pre) {
-      load_row<TPR, U>((const T*)a.x + at, t, d, v.vec, x);
-      load_row<TPR, U>((const T*)a.dy + at, t, d, v.vec, dy);
-    } else {
-      fill_row<U>(x, 0.f);
-    }
-    if (a.block) load_row<TPR, U>((const T*)a.block + at, t, d, v.vec, o);
-    if (a.dres) load_row<TPR, U>((const T*)a.dres + at, t, d, v.vec, dx);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[u][i] = next.x.u[u].at(i);
+        dy[u][i] = next.dy.u[u].at(i);
+        dx[u][i] = next.dres.u[u].at(i);
+        o[u][i] = next.o.u[u].at(i);
+      }
+    if (r + 1 < r1) fetch(r + 1);
     if (a.gate && group != r / a.gate_rows) {
       group = r / a.gate_rows;
-      load_row<TPR, U>((const T*)a.gate + ((int64_t)j * groups + group) * d, t, d, v.vec, gate);
+      load_row<TPR, U, WHOLE>((const T*)a.gate + ((int64_t)j * groups + group) * d, t, d, gate);
     }
     float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
@@ -257,7 +300,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_backward(Dev v) {
     if (a.dx)
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        store8<T>((T*)a.dx + at, (u * TPR + t) * 8, d, v.vec, dx[u]);
+        store8<T, WHOLE>((T*)a.dx + at, (u * TPR + t) * 8, d, dx[u]);
     if (!a.block) continue;
     const float ro = a.post ? 1.f / sqrtf(s[2] * inv_d + a.eps) : 1.f;
     float q[1] = {0.f};
@@ -282,12 +325,12 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_backward(Dev v) {
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      store8<T>((T*)a.dblock + at, (u * TPR + t) * 8, d, v.vec, dx[u]);
+      store8<T, WHOLE>((T*)a.dblock + at, (u * TPR + t) * 8, d, dx[u]);
     // a gate row whose rows are all this worker's is done with its last one
     if (a.gate && v.s.per == 1 && ((r + 1) % a.gate_rows == 0 || r + 1 == a.n)) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        store8<T>((T*)a.dgate + ((int64_t)j * groups + group) * d, (u * TPR + t) * 8, d, v.vec,
+        store8<T, WHOLE>((T*)a.dgate + ((int64_t)j * groups + group) * d, (u * TPR + t) * 8, d,
                   dgate[u]);
       fill_row<U>(dgate, 0.f);
     }
@@ -296,16 +339,16 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_backward(Dev v) {
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int c = (u * TPR + t) * 8;
-    if (a.pre) store8<float>(p, c, d, d % 8 == 0, dpre[u]);
-    if (a.post) store8<float>(p + d, c, d, d % 8 == 0, dpost[u]);
-    if (a.gate && v.s.per > 1) store8<float>(p + 2 * d, c, d, d % 8 == 0, dgate[u]);
+    if (a.pre) store8<float, WHOLE>(p, c, d, dpre[u]);
+    if (a.post) store8<float, WHOLE>(p + d, c, d, dpost[u]);
+    if (a.gate && v.s.per > 1) store8<float, WHOLE>(p + 2 * d, c, d, dgate[u]);
   }
 }
 
-// Column sums over the workers' partial rows: 32 columns a workgroup, eight
+// Column sums over the workers' partial rows: 32 columns a workgroup, 32
 // threads a column.  blockIdx.y: 0 dpre, 1 dpost, 2 + g the gate row g.
 template <class T>
-__global__ __launch_bounds__(256) void norm_sums(Dev v) {
+__global__ __launch_bounds__(1024) void norm_sums(Dev v) {
   const NormArgs& a = v.a;
   const int j = blockIdx.z, what = blockIdx.y, x = threadIdx.x & 31, sl = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + x, d = a.d;
@@ -314,64 +357,67 @@ __global__ __launch_bounds__(256) void norm_sums(Dev v) {
   const int w0 = what < 2 ? 0 : (what - 2) * v.s.per, w1 = what < 2 ? W : w0 + v.s.per;
   const float* p = v.part + ((int64_t)j * W * 3 + min(what, 2)) * d + c;
   float s = 0.f;
-  if (c < d)
-    for (int w = w0 + sl; w < w1; w += 8) s += p[(int64_t)w * 3 * d];
-  __shared__ float sum[8][32];
+  if (c < d) {
+#pragma unroll 4
+    for (int w = w0 + sl; w < w1; w += 32) s += p[(int64_t)w * 3 * d];
+  }
+  __shared__ float sum[32][33];
   sum[sl][x] = s;
   __syncthreads();
-  if (sl || c >= d) return;
-  for (int i = 1; i < 8; ++i) s += sum[i][x];
+  // a column's 32 sums to 32 neighbouring lanes
+  s = sum[x][sl];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor(s, o);
+  const int col = blockIdx.x * 32 + sl;
+  if (x || col >= d) return;
   if (what == 0)
-    a.dpre[j * a.dpre_stride + c] = s;
+    a.dpre[j * a.dpre_stride + col] = s;
   else if (what == 1)
-    a.dpost[j * a.dpost_stride + c] = s;
+    a.dpost[j * a.dpost_stride + col] = s;
   else
-    ((T*)a.dgate)[((int64_t)j * v.s.spans + what - 2) * d + c] = (T)s;
+    ((T*)a.dgate)[((int64_t)j * v.s.spans + what - 2) * d + col] = (T)s;
 }
 
 template <class T, int TPR, int U>
 void launch(const Dev& v, bool backward, hipStream_t s) {
   const int per = threads_of(TPR) / TPR;
-  const dim3 grid((v.s.workers() + per - 1) / per, v.a.k);
+  const dim3 grid((v.s.workers() + per - 1) / per, v.a.k), block(threads_of(TPR));
+  const bool whole = v.a.d % 8 == 0;
   if (backward)
-    klaunch(norm_backward<T, TPR, U>, grid, dim3(threads_of(TPR)), 0, s, v);
+    klaunch(whole ? norm_backward<T, TPR, U, true> : norm_backward<T, TPR, U, false>, grid, block,
+            0, s, v);
   else
-    klaunch(norm_forward<T, TPR, U>, grid, dim3(threads_of(TPR)), 0, s, v);
+    klaunch(whole ? norm_forward<T, TPR, U, true> : norm_forward<T, TPR, U, false>, grid, block, 0,
+            s, v);
 }
 
-// TPR threads of U*8 columns reach d.
 template <class T>
 hipError_t run(const Dev& v, bool backward, hipStream_t s) {
   const int d = v.a.d;
-  if (d <= 64) launch<T, 8, 1>(v, backward, s);
-  else if (d <= 128) launch<T, 16, 1>(v, backward, s);
-  else if (d <= 256) launch<T, 32, 1>(v, backward, s);
-  else if (d <= 512) launch<T, 64, 1>(v, backward, s);
-  else if (d <= 1024) launch<T, 64, 2>(v, backward, s);
-  else if (d <= 2048) launch<T, 256, 1>(v, backward, s);
-  else if (d <= 4096) launch<T, 256, 2>(v, backward, s);
-  else if (d <= 8192) launch<T, 512, 2>(v, backward, s);
+  const Shape sh = shape_of(v.a.type, d);
+  constexpr int U = sizeof(T) == 4 ? 1 : 2;
+  if (sh.tpr == 8) launch<T, 8, 1>(v, backward, s);
+  else if (sh.tpr == 16) launch<T, 16, 1>(v, backward, s);
+  else if (sh.tpr == 32) launch<T, 32, 1>(v, backward, s);
+  else if (sh.tpr == 64 && sh.u == 1) launch<T, 64, 1>(v, backward, s);
+  else if (sh.tpr == 64) launch<T, 64, U>(v, backward, s);
+  else if (sh.tpr == 128) launch<T, 128, U>(v, backward, s);
+  else if (sh.tpr == 256) launch<T, 256, U>(v, backward, s);
+  else if (sh.tpr == 512) launch<T, 512, U>(v, backward, s);
+  else if (sizeof(T) == 4 && sh.u == 1) launch<T, 1024, sizeof(T) == 4 ? 1 : 2>(v, backward, s);
   else launch<T, 1024, 2>(v, backward, s);
   if (hipError_t e = hipGetLastError()) return e;
   if (!backward || (!v.a.pre && !v.a.post && !v.a.gate)) return hipSuccess;
   const int rows = 2 + (v.a.gate && v.s.per > 1 ? v.s.spans : 0);
-  klaunch(norm_sums<T>, dim3((d + 31) / 32, rows, v.a.k), dim3(256), 0, s, v);
+  klaunch(norm_sums<T>, dim3((d + 31) / 32, rows, v.a.k), dim3(1024), 0, s, v);
   return hipGetLastError();
-}
-
-bool on_16(std::initializer_list<const void*> ps) {
-  for (const void* p : ps)
-    if ((uintptr_t)p % 16) return false;
-  return true;
 }
 
 Dev dev_of(const NormArgs& a) {
   Dev v;
   v.a = a;
   if (!a.gate) v.a.gate_rows = a.n;
-  v.s = split_rows(a.k, a.n, v.a.gate_rows);
-  v.vec = a.d % 8 == 0 && on_16({a.x, a.block, a.gate, a.x_out, a.y, a.dy, a.dres, a.dx, a.dblock,
-                                 a.dgate});
+  v.s = split_rows(a.type, a.k, a.n, a.d, v.a.gate_rows);
   v.part = (float*)a.ws;
   return v;
 }
@@ -385,8 +431,8 @@ hipError_t dispatch(const NormArgs& a, bool backward, hipStream_t s) {
 
 }  // namespace
 
-size_t norm_ws_bytes(int k, int n, int d, int gate_rows) {
-  return (size_t)k * split_rows(k, n, gate_rows).workers() * 3 * d * sizeof(float);
+size_t norm_ws_bytes(int type, int k, int n, int d, int gate_rows) {
+  return (size_t)k * split_rows(type, k, n, d, gate_rows).workers() * 3 * d * sizeof(float);
 }
 hipError_t norm_fwd(const NormArgs& a, hipStream_t s) { return dispatch(a, false, s); }
 hipError_t norm_bwd(const NormArgs& a, hipStream_t s) { return dispatch(a, true, s); }

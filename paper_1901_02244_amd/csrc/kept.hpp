@@ -70,57 +70,63 @@ __device__ __forceinline__ uint32_t abs_bits(float x) {
   return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
 }
 
-// Eight neighbouring values of a row at column c of d, as floats; zeros past
-// the row's end.  vec: 16-byte loads are allowed and d is a multiple of 8.
+// Eight neighbouring values of a row, as they lie in memory.  Rows start
+// anywhere: global loads and stores of 16 bytes need no more than their
+// element's alignment on this card, and a row that is not on 16 bytes costs
+// one more cache line a wave, where single elements cost eight loads.
 template <class T>
-__device__ __forceinline__ void load8(const T* row, int c, int d, bool vec, float (&x)[8]) {
-  if (vec) {
-    if (c < d) {
-      if constexpr (sizeof(T) == 2) {
-        typedef T v8 __attribute__((ext_vector_type(8)));
-        const v8 v = *reinterpret_cast<const v8*>(row + c);
+struct Raw8 {
+  static constexpr int WORDS = 2 * (int)sizeof(T);
+  uint32_t w[WORDS];
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (__is_same(T, float)) return __builtin_bit_cast(float, w[i]);
+    const uint32_t h = i % 2 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
+    if constexpr (__is_same(T, _Float16)) return (float)__builtin_bit_cast(_Float16, (uint16_t)h);
+    return __builtin_bit_cast(float, i % 2 ? w[i / 2] & 0xffff0000u : h << 16);
+  }
+};
+// WHOLE: d is a multiple of 8, so that no row ends inside an eight; the
+// other form's ends cost registers that the larger kernels feel.
+template <class T, bool WHOLE>
+__device__ __forceinline__ Raw8<T> load_raw8(const T* row, int c, int d) {
+  Raw8<T> r;
+  if (WHOLE ? c < d : c + 8 <= d) {
+    __builtin_memcpy(r.w, row + c, sizeof(r.w));
+    return r;
+  }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-      } else {
-        typedef float v4 __attribute__((ext_vector_type(4)));
-        const v4 a = *reinterpret_cast<const v4*>(row + c);
-        const v4 b = *reinterpret_cast<const v4*>(row + c + 4);
+  for (int i = 0; i < Raw8<T>::WORDS; ++i) r.w[i] = 0;
+  if constexpr (!WHOLE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[i] = a[i];
-          x[4 + i] = b[i];
-        }
+    for (int i = 0; i < 8; ++i)
+      if (c + i < d) {
+        if constexpr (sizeof(T) == 4)
+          r.w[i] = __builtin_bit_cast(uint32_t, row[c + i]);
+        else
+          r.w[i / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, row[c + i]) << (i % 2 * 16);
       }
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 0.f;
-    return;
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = c + i < d ? (float)row[c + i] : 0.f;
+  return r;
 }
-
-template <class T>
-__device__ __forceinline__ void store8(T* row, int c, int d, bool vec, const float (&x)[8]) {
-  if (vec) {
-    if (c >= d) return;
-    if constexpr (sizeof(T) == 2) {
-      typedef T v8 __attribute__((ext_vector_type(8)));
-      v8 v;
+// The same as floats; zeros past the row's end.
+template <class T, bool WHOLE>
+__device__ __forceinline__ void load8(const T* row, int c, int d, float (&x)[8]) {
+  const Raw8<T> r = load_raw8<T, WHOLE>(row, c, d);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = (T)x[i];
-      *reinterpret_cast<v8*>(row + c) = v;
-    } else {
-      typedef float v4 __attribute__((ext_vector_type(4)));
-      *reinterpret_cast<v4*>(row + c) = v4{x[0], x[1], x[2], x[3]};
-      *reinterpret_cast<v4*>(row + c + 4) = v4{x[4], x[5], x[6], x[7]};
-    }
-    return;
+  for (int i = 0; i < 8; ++i) x[i] = r.at(i);
+}
+template <class T, bool WHOLE>
+__device__ __forceinline__ void store8(T* row, int c, int d, const float (&x)[8]) {
+  T v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (T)x[i];
+  if (WHOLE ? c < d : c + 8 <= d) {
+    __builtin_memcpy(row + c, v, sizeof(v));
+  } else if constexpr (!WHOLE) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < d) row[c + i] = v[i];
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (c + i < d) row[c + i] = (T)x[i];
 }
 
 }  // namespace cbk

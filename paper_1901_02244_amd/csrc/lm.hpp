@@ -57,7 +57,7 @@ struct NormArgs {
   void* ws;
 };
 constexpr int NORM_MAX_D = 16384;
-size_t norm_ws_bytes(int k, int n, int d, int gate_rows);
+size_t norm_ws_bytes(int type, int k, int n, int d, int gate_rows);
 hipError_t norm_fwd(const NormArgs& a, hipStream_t s);
 hipError_t norm_bwd(const NormArgs& a, hipStream_t s);
 

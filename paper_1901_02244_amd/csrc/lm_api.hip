@@ -198,7 +198,7 @@ int cb_gated_norm_fwd(const cb_gated_norm* g, const void* x, void* x_out, void* 
 size_t cb_gated_norm_workspace_bytes(const cb_gated_norm* g) {
   if (wrong(g)) return 0;
   const NormArgs a = norm_args(g);
-  return norm_ws_bytes(a.k, a.n, a.d, a.gate_rows);
+  return norm_ws_bytes(a.type, a.k, a.n, a.d, a.gate_rows);
 }
 
 int cb_gated_norm_bwd(const cb_gated_norm* g, const void* x_out, const void* dy, const void* dres,
@@ -221,7 +221,7 @@ int cb_gated_norm_bwd(const cb_gated_norm* g, const void* x_out, const void* dy,
       return refuse(me, "dpost_stride or dpre_stride is less than d");
     if (!at(workspace_dev, 256)) return refuse(me, "workspace NULL or not on 256 bytes");
     NormArgs a = norm_args(g);
-    if (ws_bytes < norm_ws_bytes(a.k, a.n, a.d, a.gate_rows))
+    if (ws_bytes < norm_ws_bytes(a.type, a.k, a.n, a.d, a.gate_rows))
       return refuse(me, "workspace too small", CB_ENOMEM);
     a.x = g->pre ? x_out : nullptr;
     a.dy = dy;

@@ -28,6 +28,8 @@
 #pragma once
 #include "kernels.hpp"
 
+#include <atomic>
+
 namespace cbk {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -319,6 +321,24 @@ __device__ __forceinline__ void tile_of(int w, int tp, int tq, int& p, int& q) {
   const int in = id - band * BAND * tq;
   p = first + in % wide;
   q = in / wide;
+}
+
+// Launches KERNEL, which runs tiles of TL, with their LDS.  More than 64 KB
+// has to be asked for, once per kernel and device.
+template <class TL, auto KERNEL, class A>
+hipError_t launch_tile(dim3 grid, hipStream_t s, const A& a) {
+  static std::atomic<uint64_t> asked{0};
+  int dev = 0;
+  if (hipError_t e = hipGetDevice(&dev)) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(asked.load(std::memory_order_relaxed) & bit) || !bit) {
+    if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS))
+      return e;
+    asked.fetch_or(bit, std::memory_order_relaxed);
+  }
+  klaunch(KERNEL, grid, dim3(TL::THREADS), TL::LDS, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace cbk
