@@ -431,8 +431,8 @@ typedef struct {
 
 /* Workspace of the forward, or with backward != 0 of the backward call.
  * The forward's holds the counted rows and one pair of floats for each row
- * and 64 to 128 words; the backward's also the logit gradients of one piece
- * of the vocabulary (256 MB or 4096 words, whichever is more) and fp32 sums
+ * and 128 or 256 words; the backward's also the logit gradients of one piece
+ * of the vocabulary (128 MB or 4096 words, whichever is more) and fp32 sums
  * of dh.  Where rows of w do not start on 16 bytes it holds a copy of w. */
 size_t cb_vocab_xent_workspace_bytes(const cb_vocab_xent* x, int backward);
 
@@ -502,8 +502,11 @@ int cb_ckpt_unpack(int type, int64_t rows, int d, const void* kept, void* x, voi
 
 /* The weight gradient of a linear layer whose input was kept in 8 bits:
  * dw[o][c] = sum over the learner's n rows of dy[r][o] * unpacked[r][c], as
- * [out][d] with dstride elements to the next learner's (overwritten). */
-size_t cb_ckpt_wgrad_workspace_bytes(int type, int k, int n, int d, int out);
+ * [out][d] with dstride elements to the next learner's (overwritten); dy is
+ * [k*n][out].  The workspace holds fp32 sums where learners, d and out make
+ * few tiles, the unpacked rows where they make many, and a copy of dy where
+ * its rows do not start on 16 bytes. */
+size_t cb_ckpt_wgrad_workspace_bytes(int type, int k, int n, int d, int out, const void* dy);
 int cb_ckpt_wgrad(int type, int k, int n, int d, int out, const void* kept, const void* dy,
                   void* dw, int64_t dstride, void* workspace_dev, size_t ws_bytes, void* stream);
 

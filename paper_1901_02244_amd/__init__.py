@@ -183,7 +183,7 @@ def lib():
         L.cb_ckpt_pack.argtypes = [_i, _q, _i, _P, _P, _P]
         L.cb_ckpt_unpack.argtypes = [_i, _q, _i, _P, _P, _P]
         L.cb_ckpt_wgrad_workspace_bytes.restype = _z
-        L.cb_ckpt_wgrad_workspace_bytes.argtypes = [_i] * 5
+        L.cb_ckpt_wgrad_workspace_bytes.argtypes = [_i] * 5 + [_P]
         L.cb_ckpt_wgrad.argtypes = [_i] * 5 + [_P, _P, _P, _q, _P, _z, _P]
         _lib = L
     return _lib
@@ -719,7 +719,8 @@ def cb_ckpt_wgrad(kept, dy, dw=None, workspace=None, stream=None):
             dw = c.new((k, out, d), kept.dtype)
         else:
             _need(who, "dw", dw, (k, out, d), kept.dtype, dy.device, outer=True)
-        ws = c.workspace(who, lib().cb_ckpt_wgrad_workspace_bytes(code, k, n, d, out), workspace)
+        ws = c.workspace(who, lib().cb_ckpt_wgrad_workspace_bytes(code, k, n, d, out,
+                                                                   dy.data_ptr()), workspace)
         c.check(who, lib().cb_ckpt_wgrad(code, k, n, d, out, kept.data.data_ptr(), dy.data_ptr(),
                                          dw.data_ptr(), _outer(dw), ws.data_ptr(), ws.numel(),
                                          c.handle))

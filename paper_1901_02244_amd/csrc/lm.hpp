@@ -73,7 +73,7 @@ struct KeptGradArgs {
   int64_t dstride;
   void* ws;
 };
-size_t kept_grad_ws_bytes(int type, int k, int n, int d, int out);
+size_t kept_grad_ws_bytes(const KeptGradArgs& a);
 hipError_t kept_grad(const KeptGradArgs& a, hipStream_t s);
 
 }  // namespace cbk

@@ -125,6 +125,17 @@ const char* wrong_wgrad(int type, int k, int n, int d, int out) {
   return nullptr;
 }
 
+KeptGradArgs wgrad_args(int type, int k, int n, int d, int out, const void* dy) {
+  KeptGradArgs a{};
+  a.type = type;
+  a.k = k;
+  a.n = n;
+  a.d = d;
+  a.out = out;
+  a.dy = dy;
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -260,8 +271,9 @@ int cb_ckpt_unpack(int type, int64_t rows, int d, const void* kept, void* x, voi
   });
 }
 
-size_t cb_ckpt_wgrad_workspace_bytes(int type, int k, int n, int d, int out) {
-  return wrong_wgrad(type, k, n, d, out) ? 0 : kept_grad_ws_bytes(type, k, n, d, out);
+size_t cb_ckpt_wgrad_workspace_bytes(int type, int k, int n, int d, int out, const void* dy) {
+  return wrong_wgrad(type, k, n, d, out) ? 0
+                                         : kept_grad_ws_bytes(wgrad_args(type, k, n, d, out, dy));
 }
 
 int cb_ckpt_wgrad(int type, int k, int n, int d, int out, const void* kept, const void* dy,
@@ -274,16 +286,9 @@ int cb_ckpt_wgrad(int type, int k, int n, int d, int out, const void* kept, cons
       return refuse(me, "kept, dy or dw NULL or misaligned");
     if (k > 1 && dstride < (int64_t)out * d) return refuse(me, "dstride is less than out * d");
     if (!at(workspace_dev, 256)) return refuse(me, "workspace NULL or not on 256 bytes");
-    if (ws_bytes < kept_grad_ws_bytes(type, k, n, d, out))
-      return refuse(me, "workspace too small", CB_ENOMEM);
-    KeptGradArgs a;
-    a.type = type;
-    a.k = k;
-    a.n = n;
-    a.d = d;
-    a.out = out;
+    KeptGradArgs a = wgrad_args(type, k, n, d, out, dy);
+    if (ws_bytes < kept_grad_ws_bytes(a)) return refuse(me, "workspace too small", CB_ENOMEM);
     a.kept = kept;
-    a.dy = dy;
     a.dw = dw;
     a.dstride = dstride;
     a.ws = workspace_dev;

@@ -6,6 +6,13 @@
 //   row form: P[p][k] at base + p*ld + k (the contraction is contiguous);
 //   col form: P[p][k] at base + k*ld + p (the contraction is the row index).
 //
+// fp32 runs on the bf16 matrix cores, sixteen times as fast as the fp32 ones:
+// a float is exactly the sum of three bf16 numbers (its leading 8 bits, the
+// next 8 and the rest), and of the nine products of two such sums the six
+// largest are taken, which leaves out less than fp32's own rounding of the
+// product (2^-23 of it).  The split is made in registers on the way from LDS.
+// (An infinity splits into an infinity and NaNs: its products are NaN.)
+//
 // A step takes 128 bytes of contraction per row (64 elements of 16 bits or 32
 // floats) from global memory straight into LDS (buffer loads with the LDS as
 // destination, 16 bytes a lane; no registers are spent on data in flight),
@@ -45,22 +52,51 @@ __device__ __forceinline__ T from_f32(float v) {
   return (T)v;
 }
 
-// One 16x16 tile's product over 64 bytes of contraction: one MFMA of 32
-// 16-bit elements, or four of 4 floats.
+// One 16x16 tile's product over 32 elements of 16 bits.
 template <class T>
 __device__ __forceinline__ f32x4 mma(i32x4 p, i32x4 q, f32x4 c) {
-  if constexpr (__is_same(T, __bf16)) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p),
-                                                   __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
-  } else if constexpr (__is_same(T, _Float16)) {
+  if constexpr (__is_same(T, _Float16))
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, p),
                                                   __builtin_bit_cast(f16x8, q), c, 0, 0, 0);
-  } else {
-    const f32x4 a = __builtin_bit_cast(f32x4, p), b = __builtin_bit_cast(f32x4, q);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p),
+                                                   __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
+}
+
+// Eight floats as three times eight bf16 numbers whose sums they are: the
+// leading bits cut off (a rounding could pass the largest bf16), the rest
+// rounded to bf16, what then remains (at most 8 bits).
+struct Split3 {
+  i32x4 h, m, l;
+};
+__device__ __forceinline__ Split3 split3(i32x4 a, i32x4 b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  Split3 r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
-    return c;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x0 = i < 2 ? a[2 * i] : b[2 * i - 4], x1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+    r.h[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302);
+    const f32x2 rest = {
+        __builtin_bit_cast(float, x0) - __builtin_bit_cast(float, x0 & 0xffff0000u),
+        __builtin_bit_cast(float, x1) - __builtin_bit_cast(float, x1 & 0xffff0000u)};
+    const uint32_t m = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
+    r.m[i] = m;
+    const float l0 = rest[0] - __builtin_bit_cast(float, m << 16);
+    const float l1 = rest[1] - __builtin_bit_cast(float, m & 0xffff0000u);
+    r.l[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, l1),
+                                   __builtin_bit_cast(uint32_t, l0), 0x07060302);
   }
+  return r;
+}
+// The six largest products, the smallest first.
+__device__ __forceinline__ f32x4 mma3(const Split3& p, const Split3& q, f32x4 c) {
+  c = mma<__bf16>(p.m, q.m, c);
+  c = mma<__bf16>(p.l, q.h, c);
+  c = mma<__bf16>(p.h, q.l, c);
+  c = mma<__bf16>(p.m, q.h, c);
+  c = mma<__bf16>(p.h, q.m, c);
+  return mma<__bf16>(p.h, q.h, c);
 }
 
 // A buffer descriptor as the four scalar registers that inline asm takes.
@@ -107,6 +143,14 @@ struct Operand {
   int k;
 };
 
+// The permutation of a col form's 16-byte chunks in row `row` of CPR chunks:
+// of 16 rows, 0-3 and 8-11 (and 4-7 and 12-15), which half a wave reads
+// together, land in eight different 32-byte columns.
+template <int CPR>
+__device__ __forceinline__ int col_swizzle(int row) {
+  return (2 * ((row & 3) | (((row >> 3) & 1) << 2))) & (CPR - 1);
+}
+
 template <class T, int R, bool COL, int THREADS>
 struct Loader {
   static constexpr int BK = 128 / (int)sizeof(T);
@@ -122,12 +166,10 @@ struct Loader {
   uint32_t chunk;         // row form: this lane's byte in the step's 128
   int k_left;             // row form: valid bytes of contraction left
 
-  // The swizzle of chunk pairs in col form: rows 0-3, 8-11 (and 4-7, 12-15)
-  // of 16 land in eight different 32-byte columns.
   static __device__ __forceinline__ int swz(int row) {
     if constexpr (!COL) return row & 7;
     if constexpr (sizeof(T) == 4) return 0;
-    return (2 * ((row & 3) | (((row >> 3) & 1) << 2))) & (CPR - 1);
+    return col_swizzle<CPR>(row);
   }
 
   __device__ __forceinline__ void init(const Operand<T>& o, int row0, int k0, int tid) {
@@ -167,33 +209,50 @@ struct Loader {
   }
 };
 
-// A wave's operands of one half step (64 bytes of contraction) for its tiles.
+// One tile's 16-bit operand out of col form: eight k of one p a lane, the first
+// four from rows k0.., the others `apart` rows on.
+template <int R>
+__device__ __forceinline__ i32x4 read_transposed(const lds_char* lds, int r0, int k0, int apart,
+                                                 int lane) {
+  constexpr int PITCH = R * 2, CPR = PITCH / 16;
+  const int j = lane & 15;
+  i32x4 f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int row = k0 + apart * u + (j >> 2);
+    const int c = (r0 / 8 + ((j & 3) >> 1)) ^ col_swizzle<CPR>(row);
+    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s16x4*)(lds + row * PITCH + c * 16 + (j & 1) * 8));
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    f[2 * u] = (int)(uint32_t)b;
+    f[2 * u + 1] = (int)(uint32_t)(b >> 32);
+  }
+  return f;
+}
+
+// The operand of the 16 rows from r0 for half a step (64 bytes of
+// contraction): 16-bit types in either form, fp32 in row form.
+template <class T, int R, bool COL>
+__device__ __forceinline__ i32x4 read_frag(const lds_char* lds, int r0, int kk, int lane) {
+  const int g = lane >> 4, j = lane & 15;
+  if constexpr (COL) {
+    static_assert(sizeof(T) == 2, "");
+    return read_transposed<R>(lds, r0, kk * 32 + 8 * g, 4, lane);
+  } else {
+    return *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(
+        lds + (r0 + j) * 128 + (((kk * 4 + g) ^ (j & 7)) * 16));
+  }
+}
+
+// The operands of TILES tiles.
 template <class T, int R, bool COL, int TILES>
 __device__ __forceinline__ void read_frags(const lds_char* lds, int r0, int kk, int lane,
                                            i32x4 (&f)[TILES]) {
-  const int g = lane >> 4, j = lane & 15;
-  if constexpr (!COL) {
-    const lds_char* p = lds + (r0 + j) * 128 + (((kk * 4 + g) ^ (j & 7)) * 16);
+  if constexpr (!COL || sizeof(T) == 2) {
 #pragma unroll
-    for (int t = 0; t < TILES; ++t)
-      f[t] = *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(p + t * 2048);
-  } else if constexpr (sizeof(T) == 2) {
-    constexpr int PITCH = R * 2, CPR = PITCH / 16;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int row = kk * 32 + 8 * g + 4 * u + (j >> 2);
-      const int s = (2 * ((row & 3) | (((row >> 3) & 1) << 2))) & (CPR - 1);
-#pragma unroll
-      for (int t = 0; t < TILES; ++t) {
-        const int c = (r0 / 8 + 2 * t + ((j & 3) >> 1)) ^ s;
-        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(lds + row * PITCH + c * 16 + (j & 1) * 8));
-        const uint64_t b = __builtin_bit_cast(uint64_t, v);
-        f[t][2 * u] = (int)(uint32_t)b;
-        f[t][2 * u + 1] = (int)(uint32_t)(b >> 32);
-      }
-    }
+    for (int t = 0; t < TILES; ++t) f[t] = read_frag<T, R, COL>(lds, r0 + t * 16, kk, lane);
   } else {
+    const int g = lane >> 4, j = lane & 15;
     constexpr int PITCH = R * 4;
     static_assert(TILES % 4 == 0, "four interleaved tiles at a time");
 #pragma unroll
@@ -208,6 +267,33 @@ __device__ __forceinline__ void read_frags(const lds_char* lds, int r0, int kk, 
       }
     }
   }
+}
+
+// Half a step's MFMAs for 16-bit types, while the next half's operands come
+// from LDS: Q's beside, P's one by one over those that are done with, a few
+// MFMAs between the reads.  VALU: how many vector instructions of
+// what the caller does next to spread over the MFMAs too.
+template <class T, int RP, bool PCOL, int RQ, bool QCOL, int VALU, int TP, int TQ>
+__device__ __forceinline__ void half_step(f32x4 (&acc)[TP][TQ], i32x4 (&fp)[TP], i32x4 (&fq)[TQ],
+                                          const lds_char* p, const lds_char* q, int wp, int wq,
+                                          int kk, int lane) {
+  i32x4 nq[TQ];
+  read_frags<T, RQ, QCOL, TQ>(q, wq, kk, lane, nq);
+#pragma unroll
+  for (int a = 0; a < TP; ++a) {
+#pragma unroll
+    for (int b = 0; b < TQ; ++b) acc[a][b] = mma<T>(fp[a], fq[b], acc[a][b]);
+    fp[a] = read_frag<T, RP, PCOL>(p, wp + a * 16, kk, lane);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x100, QCOL ? 2 * TQ : TQ, 0);
+#pragma unroll
+  for (int a = 0; a < TP; ++a) {
+    __builtin_amdgcn_sched_group_barrier(0x8, TQ, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, PCOL ? 2 : 1, 0);
+    if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x2, VALU / TP, 0);
+  }
+#pragma unroll
+  for (int b = 0; b < TQ; ++b) fq[b] = nq[b];
 }
 
 // Tile geometry: BP x BQ by WP x WQ waves.
@@ -253,32 +339,57 @@ struct Tile {
       lp.issue(la + STAGE);
       lq.issue(la + STAGE + BP * 128);
     }
-    i32x4 fp[2][TP], fq[2][TQ];
-    read_frags<T, BP, PCOL, TP>(l, wp, 0, lane, fp[0]);
-    read_frags<T, BQ, QCOL, TQ>(l + BP * 128, wq, 0, lane, fq[0]);
-    // Half a step's operands are read while the other half's MFMAs run; the
-    // barrier between the halves finds MFMAs on both sides of it.
-    for (int s = 0; s < steps; ++s) {
-      const uint32_t cur = (s & 1) * STAGE, nxt = STAGE - cur;
-      read_frags<T, BP, PCOL, TP>(l + cur, wp, 1, lane, fp[1]);
-      read_frags<T, BQ, QCOL, TQ>(l + cur + BP * 128, wq, 1, lane, fq[1]);
-#pragma unroll
-      for (int a = 0; a < TP; ++a)
-#pragma unroll
-        for (int b = 0; b < TQ; ++b) acc[a][b] = mma<T>(fp[0][a], fq[0][b], acc[a][b]);
-      tile_wait_barrier();
-      if (s + 2 < steps) {
-        lp.issue(la + cur);
-        lq.issue(la + cur + BP * 128);
+    if constexpr (sizeof(T) == 2) {
+      i32x4 fp[TP], fq[TQ];
+      read_frags<T, BP, PCOL, TP>(l, wp, 0, lane, fp);
+      read_frags<T, BQ, QCOL, TQ>(l + BP * 128, wq, 0, lane, fq);
+      // The barrier between the halves finds MFMAs on both sides of it.  (The
+      // last step reads on into the other buffer's leftovers, for nothing.)
+      for (int s = 0; s < steps; ++s) {
+        const uint32_t cur = (s & 1) * STAGE, nxt = STAGE - cur;
+        half_step<T, BP, PCOL, BQ, QCOL, 0>(acc, fp, fq, l + cur, l + cur + BP * 128, wp, wq,
+                                                 1, lane);
+        tile_wait_barrier();
+        if (s + 2 < steps) {
+          lp.issue(la + cur);
+          lq.issue(la + cur + BP * 128);
+        }
+        half_step<T, BP, PCOL, BQ, QCOL, 0>(acc, fp, fq, l + nxt, l + nxt + BP * 128, wp, wq,
+                                                 0, lane);
       }
-      if (s + 1 < steps) {
-        read_frags<T, BP, PCOL, TP>(l + nxt, wp, 0, lane, fp[0]);
-        read_frags<T, BQ, QCOL, TQ>(l + nxt + BP * 128, wq, 0, lane, fq[0]);
+    } else {
+      // A whole step's floats are split, then the next step's are read from
+      // LDS while the MFMAs run.
+      i32x4 fp[2][TP], fq[2][TQ];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        read_frags<T, BP, PCOL, TP>(l, wp, kk, lane, fp[kk]);
+        read_frags<T, BQ, QCOL, TQ>(l + BP * 128, wq, kk, lane, fq[kk]);
       }
+      for (int s = 0; s < steps; ++s) {
+        const uint32_t cur = (s & 1) * STAGE, nxt = STAGE - cur;
+        Split3 sp[TP], sq[TQ];
 #pragma unroll
-      for (int a = 0; a < TP; ++a)
+        for (int a = 0; a < TP; ++a) sp[a] = split3(fp[0][a], fp[1][a]);
 #pragma unroll
-        for (int b = 0; b < TQ; ++b) acc[a][b] = mma<T>(fp[1][a], fq[1][b], acc[a][b]);
+        for (int b = 0; b < TQ; ++b) sq[b] = split3(fq[0][b], fq[1][b]);
+        tile_wait_barrier();
+        if (s + 2 < steps) {
+          lp.issue(la + cur);
+          lq.issue(la + cur + BP * 128);
+        }
+        if (s + 1 < steps) {
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            read_frags<T, BP, PCOL, TP>(l + nxt, wp, kk, lane, fp[kk]);
+            read_frags<T, BQ, QCOL, TQ>(l + nxt + BP * 128, wq, kk, lane, fq[kk]);
+          }
+        }
+#pragma unroll
+        for (int a = 0; a < TP; ++a)
+#pragma unroll
+          for (int b = 0; b < TQ; ++b) acc[a][b] = mma3(sp[a], sq[b], acc[a][b]);
+      }
     }
   }
 
@@ -310,6 +421,24 @@ struct Tile {
     return b * 16 + (lane & 15);
   }
 };
+
+// Stores four neighbouring results of T at `at`, of which `left` exist.
+template <class T>
+__device__ __forceinline__ void store4(T* at, f32x4 v, float f, int left, bool vec) {
+  T o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = from_f32<T>(v[i] * f);
+  if (vec) {
+    if constexpr (sizeof(T) == 2)
+      *(uint64_t*)at = *(const uint64_t*)o;
+    else
+      *(f32x4*)at = *(const f32x4*)o;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < left) at[i] = o[i];
+  }
+}
 
 // Tile numbers of a grid of tp x tq tiles: workgroup w of G = tp*tq takes the
 // tiles in bands of BAND tiles of p, XCD-major, so that the workgroups that

@@ -27,6 +27,7 @@
 #include "lm_tile.hpp"
 
 #include <algorithm>
+#include <climits>
 
 namespace cbk {
 namespace {
@@ -258,7 +259,8 @@ __device__ constexpr int swz_of() {
 // share.
 template <class TL, bool BACKWARD, bool EDGE>
 __device__ __forceinline__ void logits_end(const LogitArgs& a, int j, int cnt, int p0, int q0,
-                                           char* lds, typename TL::Acc& acc) {
+                                           char* lds, const int (&label)[TL::TQ],
+                                           const float (&lses)[TL::TQ], typename TL::Acc& acc) {
   using T = typename TL::T;
   const int lane = threadIdx.x & 63, lp = 4 * (lane >> 4);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -266,10 +268,8 @@ __device__ __forceinline__ void logits_end(const LogitArgs& a, int j, int cnt, i
   const int pv = a.vn - p0 - wp;  // words of this wave's share that exist
 #pragma unroll
   for (int b = 0; b < TL::TQ; ++b) {
-    const int x = wq + TL::col_of(b, lane), q = q0 + x;
-    const bool in = q < cnt;
-    const int64_t at = (int64_t)j * a.cap + q;
-    const int y = in ? a.lab[at] - a.v0 - p0 - wp : -1;  // label, from the wave's first word
+    const int x = wq + TL::col_of(b, lane);
+    const int y = label[b] - wp;  // from the wave's first word
     if constexpr (!BACKWARD) {
       float m = NEG_INF;
 #pragma unroll
@@ -286,7 +286,7 @@ __device__ __forceinline__ void logits_end(const LogitArgs& a, int j, int cnt, i
         for (int t = 0; t < TL::TP; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) l = y == t * 16 + lp + i ? acc[t][b][i] : l;
-        a.plog[at] = l;
+        a.plog[(int64_t)j * a.cap + q0 + x] = l;
       }
       m = fmaxf(m, __shfl_xor(m, 16));
       m = fmaxf(m, __shfl_xor(m, 32));
@@ -300,7 +300,7 @@ __device__ __forceinline__ void logits_end(const LogitArgs& a, int j, int cnt, i
       e += __shfl_xor(e, 32);
       if (lane < 16) reinterpret_cast<float2*>(lds)[wave / TL::WQ * TL::BQ + x] = {m, e};
     } else {
-      const float lse = in ? a.lse[(int64_t)j * a.n + a.row[at]] : 0.f;
+      const float lse = lses[b];
 #pragma unroll
       for (int t = 0; t < TL::TP; ++t) {
         T out[4];
@@ -325,7 +325,7 @@ __device__ __forceinline__ void logits_end(const LogitArgs& a, int j, int cnt, i
 }
 
 template <class TL, bool BACKWARD>
-__global__ __launch_bounds__(TL::THREADS) void xent_logits(LogitArgs a) {
+__global__ __launch_bounds__(TL::THREADS, 2) void xent_logits(LogitArgs a) {
   using T = typename TL::T;
   extern __shared__ __align__(16) char lds[];
   const int j = blockIdx.y, cnt = a.cnt[j];
@@ -336,13 +336,25 @@ __global__ __launch_bounds__(TL::THREADS) void xent_logits(LogitArgs a) {
   if (q0 >= cnt) return;
   const Operand<T> W{(const T*)a.w + j * a.pstride, a.ldw, a.vn, a.d};
   const Operand<T> H{(const T*)a.hc + (int64_t)j * a.cap * a.dp, a.dp, cnt, a.d};
+  // what the end needs of its rows is fetched behind the product: the labels,
+  // from the tile's first word (negative: no word here), and the lse
+  int label[TL::TQ];
+  float lses[TL::TQ];
+  const int wq = (threadIdx.x >> 6) % TL::WQ * TL::SQ;
+#pragma unroll
+  for (int b = 0; b < TL::TQ; ++b) {
+    const int q = q0 + wq + TL::col_of(b, threadIdx.x & 63);
+    const int64_t at = (int64_t)j * a.cap + q;
+    label[b] = q < cnt ? a.lab[at] - a.v0 - p0 : INT_MIN / 2;
+    lses[b] = BACKWARD && q < cnt ? a.lse[(int64_t)j * a.n + a.row[at]] : 0.f;
+  }
   typename TL::Acc acc;
   TL::product(W, H, p0, q0, 0, a.d, lds, acc);
   __syncthreads();  // the operands' LDS is used again
   if (p0 + TL::BP <= a.vn)
-    logits_end<TL, BACKWARD, false>(a, j, cnt, p0, q0, lds, acc);
+    logits_end<TL, BACKWARD, false>(a, j, cnt, p0, q0, lds, label, lses, acc);
   else
-    logits_end<TL, BACKWARD, true>(a, j, cnt, p0, q0, lds, acc);
+    logits_end<TL, BACKWARD, true>(a, j, cnt, p0, q0, lds, label, lses, acc);
   __syncthreads();
   if constexpr (!BACKWARD) {
     const int x = threadIdx.x;
@@ -495,27 +507,9 @@ struct DhArgs {
   float scale;
 };
 
-// Stores four neighbouring results of T at `at`, of which `left` exist.
-template <class T>
-__device__ __forceinline__ void store4(T* at, f32x4 v, float f, int left, bool vec) {
-  T o[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = from_f32<T>(v[i] * f);
-  if (vec) {
-    if constexpr (sizeof(T) == 2)
-      *(uint64_t*)at = *(const uint64_t*)o;
-    else
-      *(f32x4*)at = *(const f32x4*)o;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < left) at[i] = o[i];
-  }
-}
-
 // dh: P = W in col form (p = column), Q = g in row form (q = row).
 template <class TL>
-__global__ __launch_bounds__(TL::THREADS) void xent_dh_sums(DhArgs a) {
+__global__ __launch_bounds__(TL::THREADS, 2) void xent_dh_sums(DhArgs a) {
   using T = typename TL::T;
   extern __shared__ __align__(16) char lds[];
   const int j = blockIdx.y, cnt = a.cnt[j], s = blockIdx.z;
@@ -580,7 +574,7 @@ struct DwArgs {
 // dW rows of the piece: P = h in col form (p = column), Q = g in col form
 // (q = word).
 template <class TL>
-__global__ __launch_bounds__(TL::THREADS) void xent_dw(DwArgs a) {
+__global__ __launch_bounds__(TL::THREADS, 2) void xent_dw(DwArgs a) {
   using T = typename TL::T;
   extern __shared__ __align__(16) char lds[];
   const int j = blockIdx.y, cnt = a.cnt[j];

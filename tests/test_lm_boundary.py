@@ -137,12 +137,14 @@ def test_ckpt_refuses():
     assert L.cb_ckpt_pack(2, 4, 32, A + 1, A, None) == E and L.cb_ckpt_pack(2, 4, 32, A, A + 8, None) == E
     assert L.cb_ckpt_unpack(2, 4, 32, A + 8, A, None) == E and L.cb_ckpt_unpack(2, 4, 32, A, A + 1, None) == E
     size, w = L.cb_ckpt_wgrad_workspace_bytes, L.cb_ckpt_wgrad
-    need = size(2, 2, 16, 64, 32)
+    need = size(2, 2, 16, 64, 32, A)
     assert need > 0
     for bad in ((3, 2, 16, 64, 32), (2, 0, 16, 64, 32), (2, 2, 0, 64, 32), (2, 2, 16, 0, 32), (2, 2, 16, 64, 0),
                 (2, 2, 16, (1 << 20) + 1, 32), (2, 2, 16, 64, (1 << 20) + 1), (2, 2, 1 << 30, 64, 32)):
-        assert size(*bad) == 0
+        assert size(*bad, A) == 0
         assert w(*bad, A, A, A, 1 << 30, A, BIG, None) == E
+    # a copy of dy only where its rows do not start on 16 bytes
+    assert size(2, 1, 64, 64, 4096, A + 2) - size(2, 1, 64, 64, 4096, A) >= 64 * 4096 * 2 - 256
     ok = (2, 2, 16, 64, 32)
     assert w(*ok, None, A, A, 2048, A, BIG, None) == E and w(*ok, A, None, A, 2048, A, BIG, None) == E
     assert w(*ok, A, A, None, 2048, A, BIG, None) == E and w(*ok, A, A, A, 2047, A, BIG, None) == E
