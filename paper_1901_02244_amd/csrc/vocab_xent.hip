@@ -23,7 +23,7 @@
 // normal numbers and -1 is still in range; the scale is taken out, with s/C,
 // from the fp32 sums.  That store is the only rounding before the results'
 // own.
-#include "lm.hpp"
+#include "kept.hpp"
 #include "lm_tile.hpp"
 
 #include <algorithm>
@@ -41,58 +41,58 @@ constexpr float g_scale() {
 
 __host__ __device__ constexpr int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-struct DhShape {
-  int shape, splits;
-};
-// Places in the workspace, in bytes.
-struct Layout {
-  int cap;       // rows of a learner, up to a multiple of 64
-  int dp;        // columns of the gathered rows, up to a multiple of 128 bytes
-  int parts;     // tiles of the vocabulary, each with a (max, sum) of a row
-  int piece;     // vocabulary rows of one piece of the backward pass
-  DhShape dhs;
-  bool copy_w;
-  size_t cnt, pos, row, lab, hc, wc, part, plog, rloss, g, dh, total;
-};
-
 // Tile shapes.  THIN for up to 32 rows of a learner.  Else BIG (256 x 256,
 // one workgroup a CU) or MID (128 x 128, two), whichever needs less time for
 // the rounds that 256 CUs make of the tiles: a BIG tile is four MID ones and
 // MID_COST as dear per element, twice the LDS reads for a product.  fp32
-// takes MID always: its MFMAs are sixteen times slower, so that LDS is never
-// in the way and the smaller tile's finer rounds are free.
+// takes MID always: six MFMAs a product keep LDS out of the way, and the
+// smaller tile's finer rounds are free.
 enum { BIG, MID, THIN };
 constexpr double MID_COST = 1.3;
 
 int64_t tiles(int64_t a, int64_t b, int ba, int bb) { return up(a, ba) / ba * (up(b, bb) / bb); }
-
-int big_or_mid(int type, int64_t big, int64_t mid) {
-  if (type == LM_F32) return MID;
-  return (big + 255) / 256 * 4 <= (mid + 511) / 512 * 2 * MID_COST ? BIG : MID;
-}
-int shape_of(int type, int k, int64_t p, int64_t q) {
-  if (q <= 32) return THIN;
-  return big_or_mid(type, k * tiles(p, q, 256, 256), k * tiles(p, q, 128, 128));
-}
 int bp_of(int shape) { return shape == MID ? 128 : 256; }
 int bq_of(int shape) { return shape == BIG ? 256 : shape == MID ? 128 : 32; }
+int64_t tiles_of(int shape, int k, int64_t p, int64_t q) {
+  return k * tiles(p, q, bp_of(shape), bq_of(shape));
+}
 
-// The product for dh has few tiles and, in the vocabulary, a long sum: where
-// the tiles do not fill the CUs, `splits` workgroups share a tile's sum.
-DhShape dh_shape(int type, int k, int n, int d, int words) {
+// How a product of k learners' p x q over `sum` terms is cut.  Where the
+// tiles do not fill the CUs, `splits` workgroups share a tile's sum, and a
+// kernel after it adds up what they leave in the workspace.
+struct Plan {
+  int shape, splits;
+};
+Plan plan(int type, int k, int64_t p, int64_t q, int64_t sum, bool thin, bool big_splits) {
   const int bk = 128 / lm_size(type);
-  const int64_t steps = up(words, bk) / bk;
-  if (n <= 32 || type == LM_F32) {
-    const int sh = n <= 32 ? THIN : MID;
-    const int64_t t = k * tiles(d, n, bp_of(sh), bq_of(sh));
-    return {sh, (int)std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / 4))};
+  const int64_t steps = up(sum, bk) / bk;
+  // from twelve steps on: the adding up is a launch more, as long as some steps
+  auto share = [&](int64_t slots, int64_t t, int least) {
+    return steps < 12 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(slots / t, steps / least));
+  };
+  if (thin && q <= 32) return {THIN, share(512, tiles_of(THIN, k, p, q), 4)};
+  const int64_t mid = tiles_of(MID, k, p, q), big = tiles_of(BIG, k, p, q);
+  if (type != LM_F32) {
+    if (mid > 256 && (big + 255) / 256 * 4 <= (mid + 511) / 512 * 2 * MID_COST) return {BIG, 1};
+    const int s = share(256, big, 8);
+    if (big_splits && s > 1 && big * s >= 128) return {BIG, s};
   }
-  const int64_t t = k * tiles(d, n, 256, 256);
-  if (t >= 256) return {BIG, 1};
-  const int64_t s = std::max<int64_t>(1, std::min<int64_t>(256 / t, steps / 8));
-  if (t * s >= 128) return {BIG, (int)s};
-  const int64_t m = k * tiles(d, n, 128, 128);
-  return {MID, (int)std::max<int64_t>(1, std::min<int64_t>(512 / m, steps / 4))};
+  return {MID, share(512, mid, 4)};
+}
+
+// Places in the workspace, in bytes.
+struct Layout {
+  int cap;       // rows of a learner, up to a multiple of 64
+  int dp;        // columns of the gathered rows, up to a multiple of 128 bytes
+  int piece;     // vocabulary rows of one piece of the backward pass
+  int parts;     // tiles of the vocabulary, each with a (max, sum) of a row
+  Plan logits, dh, dw;
+  bool copy_w;
+  size_t cnt, pos, row, lab, hc, wc, part, plog, rloss, g, lsum, dhsum, dwsum, total;
+};
+
+Plan plan_logits(int type, int k, int n, int d, int v) {
+  return plan(type, k, v, n, d, true, false);
 }
 
 Layout layout(const XentArgs& a, bool backward) {
@@ -103,7 +103,6 @@ Layout layout(const XentArgs& a, bool backward) {
   // the rows of W are read 16 bytes at a time
   l.copy_w = (uintptr_t)a.w % 16 || (int64_t)d * sz % 16 || (k > 1 && a.pstride * sz % 16);
   const int64_t rows = (int64_t)k * l.cap;
-  l.parts = (int)(up(v, bp_of(shape_of(a.type, k, v, n))) / bp_of(shape_of(a.type, k, v, n)));
   // A piece's g takes up to 128 MB, so that it and the piece of W stay in the
   // 256 MB of the memory-side cache between the products (8192 rows of 4096,
   // 128,000 words in bf16: 25.1 ms, with 256 MB 25.8, with 512 MB 25.3), but
@@ -111,7 +110,12 @@ Layout layout(const XentArgs& a, bool backward) {
   // a piece stays small beside the products.
   const int64_t fit = (int64_t(128) << 20) / (rows * sz) / 256 * 256;
   l.piece = (int)std::min<int64_t>(up(v, 256), std::max<int64_t>(4096, fit));
-  l.dhs = dh_shape(a.type, k, n, d, std::min(l.piece, v));
+  l.logits = plan_logits(a.type, k, n, d, v);
+  l.parts = (int)(up(v, bp_of(l.logits.shape)) / bp_of(l.logits.shape));
+  l.dh = plan(a.type, k, d, n, std::min(l.piece, v), true, true);
+  l.dw = plan(a.type, k, d, std::min(l.piece, v), n, false, true);
+  // logits in shares only where they are few, which are one piece
+  if (v > l.piece) l.logits.splits = 1;
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t here = at;
@@ -124,11 +128,13 @@ Layout layout(const XentArgs& a, bool backward) {
   l.lab = take(rows * 4);
   l.hc = take(rows * l.dp * sz);
   l.wc = l.copy_w ? take((int64_t)k * v * l.dp * sz) : 0;
-  l.part = l.plog = l.rloss = l.g = l.dh = 0;
+  l.part = l.plog = l.rloss = l.g = l.lsum = l.dhsum = l.dwsum = 0;
+  if (l.logits.splits > 1) l.lsum = take(l.logits.splits * rows * up(v, 256) * 4);
   if (backward) {
     l.g = take(rows * l.piece * sz);
-    // not where one product writes dh itself
-    if (l.dhs.splits > 1 || l.piece < v) l.dh = take((int64_t)l.dhs.splits * rows * l.dp * 4);
+    // not where one product writes the result itself
+    if (l.dh.splits > 1 || l.piece < v) l.dhsum = take(l.dh.splits * rows * l.dp * 4);
+    if (l.dw.splits > 1) l.dwsum = take((int64_t)l.dw.splits * k * std::min(l.piece, v) * l.dp * 4);
   } else {
     l.part = take((int64_t)l.parts * rows * 8);
     l.plog = take(rows * 4);
@@ -139,8 +145,6 @@ Layout layout(const XentArgs& a, bool backward) {
 }
 
 // --- the counted rows ----------------------------------------------------------
-
-constexpr int ROWS_PER_BLOCK = 16;
 
 struct RowsArgs {
   const void* h;
@@ -153,16 +157,17 @@ struct RowsArgs {
 };
 
 // Gathers the counted rows of a learner, in order: every workgroup counts the
-// labels before its own 16 rows (n/16 workgroups reading up to n labels from
-// L2 cost less than a second launch), then copies its rows, padded with zeros
-// to dp columns.  pos[r] is the gathered place of row r or -1, row[] and
-// lab[] its inverse and the labels there.
-template <class T, bool VEC>
+// labels before its own R rows (n/R workgroups reading up to n labels from L2
+// cost less than a second launch), then its four waves copy rows, padded with
+// zeros to dp columns.  pos[r] is the gathered place of row r or -1, row[]
+// and lab[] its inverse and the labels there.
+template <class T, int R>
 __global__ __launch_bounds__(256) void xent_rows(RowsArgs a) {
-  const int j = blockIdx.y, r0 = blockIdx.x * ROWS_PER_BLOCK, tid = threadIdx.x;
+  const int j = blockIdx.y, r0 = blockIdx.x * R, tid = threadIdx.x;
   const int32_t* lab = a.labels + (int64_t)j * a.n;
-  __shared__ int wave_sum[4], place[ROWS_PER_BLOCK];
+  __shared__ int wave_sum[4], place[R];
   int c = 0;
+#pragma unroll 4
   for (int i = tid; i < r0; i += 256) c += lab[i] != a.ignore;
 #pragma unroll
   for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
@@ -171,7 +176,7 @@ __global__ __launch_bounds__(256) void xent_rows(RowsArgs a) {
   const int before = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
   if (tid < 64) {
     const int r = r0 + tid;
-    const bool mine = tid < ROWS_PER_BLOCK && r < a.n;
+    const bool mine = tid < R && r < a.n;
     const int y = mine ? lab[r] : a.ignore;
     const uint64_t m = __ballot(y != a.ignore);
     const int p = before + __popcll(m & ((1ull << tid) - 1));
@@ -184,32 +189,24 @@ __global__ __launch_bounds__(256) void xent_rows(RowsArgs a) {
         a.lab[(int64_t)j * a.cap + p] = y;
       }
     }
-    if (tid == 0 && r0 + ROWS_PER_BLOCK >= a.n) {
-      a.cnt[j] = before + __popcll(m);
-    }
+    if (tid == 0 && r0 + R >= a.n) a.cnt[j] = before + __popcll(m);
   }
   __syncthreads();
   const int lane = tid & 63;
-  for (int i = tid >> 6; i < ROWS_PER_BLOCK && r0 + i < a.n; i += 4) {
+  for (int i = tid >> 6; i < R && r0 + i < a.n; i += 4) {
     const int p = place[i];
-    if (p < 0) {
-      if (a.dh) {
-        T* out = (T*)a.dh + ((int64_t)j * a.n + r0 + i) * a.d;
-        for (int x = lane; x < a.d; x += 64) out[x] = (T)0.f;
+    const int64_t r = (int64_t)j * a.n + r0 + i;
+    const float zeros[8] = {};
+    if (p >= 0) {
+      const T* src = (const T*)a.h + r * a.ldh;
+      T* dst = (T*)a.hc + ((int64_t)j * a.cap + p) * a.dp;
+#pragma unroll 4
+      for (int x = lane * 8; x < a.dp; x += 512) {
+        const Raw8<T> v = load_raw8<T, false>(src, x, a.d);
+        __builtin_memcpy(dst + x, v.w, sizeof(v.w));
       }
-      continue;
-    }
-    const T* src = (const T*)a.h + ((int64_t)j * a.n + r0 + i) * a.ldh;
-    T* dst = (T*)a.hc + ((int64_t)j * a.cap + p) * a.dp;
-    if constexpr (VEC) {
-      constexpr int E = 16 / sizeof(T);
-      for (int x = lane * E; x < a.dp; x += 64 * E) {
-        i32x4 v = {0, 0, 0, 0};
-        if (x < a.d) v = *(const i32x4*)(src + x);
-        *(i32x4*)(dst + x) = v;
-      }
-    } else {
-      for (int x = lane; x < a.dp; x += 64) dst[x] = x < a.d ? src[x] : (T)0.f;
+    } else if (a.dh) {
+      for (int x = lane * 8; x < a.d; x += 512) store8<T, false>((T*)a.dh + r * a.d, x, a.d, zeros);
     }
   }
 }
@@ -219,24 +216,32 @@ __global__ __launch_bounds__(256) void xent_rows(RowsArgs a) {
 template <class T>
 __global__ __launch_bounds__(256) void xent_copy_w(const T* w, int64_t pstride, int v, int d,
                                                    int dp, T* wc) {
-  const int j = blockIdx.y, lane = threadIdx.x & 63;
-  for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < v; r += gridDim.x * 4) {
-    const T* src = w + j * pstride + (int64_t)r * d;
-    T* dst = wc + ((int64_t)j * v + r) * dp;
-    for (int x = lane; x < dp; x += 64) dst[x] = x < d ? src[x] : (T)0.f;
+  const int j = blockIdx.y;
+  const int64_t units = (int64_t)v * (dp / 8);
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < units; i += gridDim.x * 256ll) {
+    const int64_t r = i / (dp / 8);
+    const int c = (int)(i - r * (dp / 8)) * 8;
+    const Raw8<T> x = load_raw8<T, false>(w + j * pstride + r * d, c, d);
+    __builtin_memcpy(wc + ((int64_t)j * v + r) * dp + c, x.w, sizeof(x.w));
   }
 }
 
 // --- logits --------------------------------------------------------------------
+
+// What xent_logits leaves: the pairs of the loss, g, or a split's sums.
+enum { LOSS, GRAD, SUMS };
 
 struct LogitArgs {
   const void* w;    // replica 0's first row of the vocabulary range
   int64_t ldw, pstride;
   int d;            // width of W's rows that holds values
   int v0, vn;       // the vocabulary range [v0, v0 + vn)
-  const void* hc;
-  int dp, cap;
-  const int *cnt, *lab, *row;
+  const void* hc;   // rows dp apart, a learner's hstride
+  int64_t dp, hstride;
+  int cap;
+  const int *cnt;   // counted rows, or nullptr: n
+  const int *lab, *row;
+  int ldlab;        // labels of a learner apart
   // forward
   float2* part;     // [k][parts][cap]
   float* plog;      // [k][cap]
@@ -246,6 +251,10 @@ struct LogitArgs {
   int n;
   void* g;          // [k][cap][ldg]
   int ldg;
+  // splits of the columns, `span` each
+  float* sums;      // [splits][k][cap][lds]
+  int lds, span;
+  int64_t split_stride;
 };
 
 // Which bits of a row's number permute its chunks in LDS: at most a row's.
@@ -257,7 +266,7 @@ __device__ constexpr int swz_of() {
 
 // What a tile's logits become.  EDGE: the vocabulary ends inside the wave's
 // share.
-template <class TL, bool BACKWARD, bool EDGE>
+template <class TL, int MODE, bool EDGE>
 __device__ __forceinline__ void logits_end(const LogitArgs& a, int j, int cnt, int p0, int q0,
                                            char* lds, const int (&label)[TL::TQ],
                                            const float (&lses)[TL::TQ], typename TL::Acc& acc) {
@@ -270,7 +279,7 @@ __device__ __forceinline__ void logits_end(const LogitArgs& a, int j, int cnt, i
   for (int b = 0; b < TL::TQ; ++b) {
     const int x = wq + TL::col_of(b, lane);
     const int y = label[b] - wp;  // from the wave's first word
-    if constexpr (!BACKWARD) {
+    if constexpr (MODE == LOSS) {
       float m = NEG_INF;
 #pragma unroll
       for (int t = 0; t < TL::TP; ++t)
@@ -324,18 +333,28 @@ __device__ __forceinline__ void logits_end(const LogitArgs& a, int j, int cnt, i
   }
 }
 
-template <class TL, bool BACKWARD>
+template <class TL, int MODE>
 __global__ __launch_bounds__(TL::THREADS, 2) void xent_logits(LogitArgs a) {
   using T = typename TL::T;
   extern __shared__ __align__(16) char lds[];
-  const int j = blockIdx.y, cnt = a.cnt[j];
+  const int j = blockIdx.y, cnt = a.cnt ? a.cnt[j] : a.n;
   const int np = (a.vn + TL::BP - 1) / TL::BP;
   int tp, tq;
   tile_of<8>(blockIdx.x, np, gridDim.x / np, tp, tq);
   const int p0 = tp * TL::BP, q0 = tq * TL::BQ;
   if (q0 >= cnt) return;
   const Operand<T> W{(const T*)a.w + j * a.pstride, a.ldw, a.vn, a.d};
-  const Operand<T> H{(const T*)a.hc + (int64_t)j * a.cap * a.dp, a.dp, cnt, a.d};
+  const Operand<T> H{(const T*)a.hc + j * a.hstride, a.dp, cnt, a.d};
+  typename TL::Acc acc;
+  if constexpr (MODE == SUMS) {
+    const int s = blockIdx.z;
+    TL::product(W, H, p0, q0, min(s * a.span, a.d), min((s + 1) * a.span, a.d), lds, acc);
+    float* out = a.sums + s * a.split_stride + ((int64_t)j * a.cap + q0) * a.lds + p0;
+    TL::for_each_quad(acc, [&](int p, int q, f32x4 v) {
+      if (q0 + q < cnt) *(f32x4*)(out + (int64_t)q * a.lds + p) = v;
+    });
+    return;
+  }
   // what the end needs of its rows is fetched behind the product: the labels,
   // from the tile's first word (negative: no word here), and the lse
   int label[TL::TQ];
@@ -345,18 +364,17 @@ __global__ __launch_bounds__(TL::THREADS, 2) void xent_logits(LogitArgs a) {
   for (int b = 0; b < TL::TQ; ++b) {
     const int q = q0 + wq + TL::col_of(b, threadIdx.x & 63);
     const int64_t at = (int64_t)j * a.cap + q;
-    label[b] = q < cnt ? a.lab[at] - a.v0 - p0 : INT_MIN / 2;
-    lses[b] = BACKWARD && q < cnt ? a.lse[(int64_t)j * a.n + a.row[at]] : 0.f;
+    label[b] = q < cnt ? a.lab[(int64_t)j * a.ldlab + q] - a.v0 - p0 : INT_MIN / 2;
+    lses[b] = MODE == GRAD && q < cnt ? a.lse[(int64_t)j * a.n + a.row[at]] : 0.f;
   }
-  typename TL::Acc acc;
   TL::product(W, H, p0, q0, 0, a.d, lds, acc);
   __syncthreads();  // the operands' LDS is used again
   if (p0 + TL::BP <= a.vn)
-    logits_end<TL, BACKWARD, false>(a, j, cnt, p0, q0, lds, label, lses, acc);
+    logits_end<TL, MODE, false>(a, j, cnt, p0, q0, lds, label, lses, acc);
   else
-    logits_end<TL, BACKWARD, true>(a, j, cnt, p0, q0, lds, label, lses, acc);
+    logits_end<TL, MODE, true>(a, j, cnt, p0, q0, lds, label, lses, acc);
   __syncthreads();
-  if constexpr (!BACKWARD) {
+  if constexpr (MODE == LOSS) {
     const int x = threadIdx.x;
     if (x < TL::BQ && q0 + x < cnt) {
       const float2* l = reinterpret_cast<const float2*>(lds) + x;
@@ -392,9 +410,12 @@ __device__ __forceinline__ void join(float& m, float& e, float m2, float e2) {
 }
 
 struct JoinArgs {
+  // the gathered rows' count, places and labels; or cnt and pos nullptr, lab
+  // the labels themselves (cap labels of a learner apart from the next one's)
   const int *cnt, *pos, *lab;
+  int ignore, ldlab;
   const float2* part;
-  const float* plog;
+  float* plog;
   int parts, cap, n, v;
   float *lse, *rloss;
   float* loss;      // one workgroup a learner: the mean too; else nullptr
@@ -404,6 +425,7 @@ struct JoinArgs {
 __device__ __forceinline__ double block_sum(double t) {
   __shared__ double sum[256];
   const int tid = threadIdx.x;
+  __syncthreads();
   sum[tid] = t;
   __syncthreads();
   for (int o = 128; o; o >>= 1) {
@@ -413,19 +435,124 @@ __device__ __forceinline__ double block_sum(double t) {
   return sum[0];
 }
 
-// Stores a row's lse and returns its loss; 0 and no loss where the label is
-// ignored (p < 0).
+// The place of row r, or -1.
+__device__ __forceinline__ int place_of(const JoinArgs& a, int j, int r) {
+  if (a.pos) return a.pos[(int64_t)j * a.n + r];
+  return a.lab[(int64_t)j * a.ldlab + r] != a.ignore ? r : -1;
+}
+
+// Stores a row's lse and returns its loss, given the label's logit; 0 and no
+// loss where the label is ignored (p < 0).
 __device__ __forceinline__ float row_loss(const JoinArgs& a, int j, int r, int p, float m,
-                                          float e) {
+                                          float e, float logit) {
   float out = 0.f, loss = 0.f;
   if (p >= 0) {
     out = (m == NEG_INF ? 0.f : m) + logf(e);
-    const int y = a.lab[(int64_t)j * a.cap + p];
-    loss = y >= 0 && y < a.v ? out - a.plog[(int64_t)j * a.cap + p] : __builtin_nanf("");
+    const int y = a.lab[(int64_t)j * a.ldlab + p];
+    loss = y >= 0 && y < a.v ? out - logit : __builtin_nanf("");
   }
   a.lse[(int64_t)j * a.n + r] = out;
   a.rloss[(int64_t)j * a.n + r] = loss;
   return loss;
+}
+
+// The splits' sums of four neighbouring logits, added in order.
+__device__ __forceinline__ f32x4 sum4(const float* at, int splits, int64_t stride) {
+  f32x4 v = *(const f32x4*)at;
+#pragma unroll 4
+  for (int s = 1; s < splits; ++s) v += *(const f32x4*)(at + s * stride);
+  return v;
+}
+
+struct SumArgs {
+  JoinArgs o;
+  const float* sums;
+  int splits, lds;
+  int64_t split_stride;
+  // backward
+  const float* lse;
+  const int* row;
+  void* g;
+  int ldg;
+};
+
+// Where splits share the logits' sums, the loss from those sums: WIDE, a
+// workgroup a row, else a wave a row, and with loss one workgroup takes all
+// rows of a learner and their mean.
+template <bool WIDE>
+__global__ __launch_bounds__(256) void xent_sums_loss(SumArgs a) {
+  const JoinArgs& o = a.o;
+  const int j = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  constexpr int R = WIDE ? 1 : 4, S = 256 / R;
+  const int s = tid % S;
+  __shared__ float3 shares[4];
+  double total = 0.0, rows = 0.0;
+  for (int r = blockIdx.x * R + tid / S; r < o.n; r += gridDim.x * R) {
+    const int p = place_of(o, j, r);
+    float m = NEG_INF, e = 0.f, l = 0.f;  // l: the label's logit, if it is this lane's
+    if (p >= 0) {
+      const float* at = a.sums + ((int64_t)j * o.cap + p) * a.lds;
+      const int y = o.lab[(int64_t)j * o.ldlab + p];
+      for (int v = s * 4; v < o.v; v += S * 4) {
+        const f32x4 x = sum4(at + v, a.splits, a.split_stride);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (v + i >= o.v) continue;
+          join(m, e, x[i], 1.f);
+          if (v + i == y) l = x[i];
+        }
+      }
+#pragma unroll
+      for (int b = 32; b; b >>= 1) {
+        join(m, e, __shfl_xor(m, b), __shfl_xor(e, b));
+        l += __shfl_xor(l, b);
+      }
+    }
+    if constexpr (WIDE) {
+      if (lane == 0) shares[tid >> 6] = {m, e, l};
+      __syncthreads();
+      if (tid == 0) {
+        for (int i = 1; i < 4; ++i) {
+          join(m, e, shares[i].x, shares[i].y);
+          l += shares[i].z;
+        }
+        row_loss(o, j, r, p, m, e, l);
+      }
+      __syncthreads();
+    } else {
+      if (lane == 0) {
+        total += row_loss(o, j, r, p, m, e, l);
+        rows += p >= 0;
+      }
+    }
+  }
+  if (!o.loss) return;
+  total = block_sum(total);
+  rows = block_sum(rows);
+  if (tid == 0) o.loss[j] = (float)(total / fmax(rows, 1.0));
+}
+
+// and g: S threads a row; zeros up to the next 128 words.
+template <class T, int S>
+__global__ __launch_bounds__(256) void xent_sums_grad(SumArgs a) {
+  const JoinArgs& o = a.o;
+  const int j = blockIdx.y, s = threadIdx.x % S;
+  const int q = blockIdx.x * (256 / S) + threadIdx.x / S;
+  if (q >= o.cnt[j]) return;
+  const int64_t at = (int64_t)j * o.cap + q;
+  const int y = o.lab[at];
+  const float lse = a.lse[(int64_t)j * o.n + a.row[at]];
+  const int end = (o.v + 127) / 128 * 128;
+  for (int v = s * 4; v < end; v += S * 4) {
+    f32x4 g = {0.f, 0.f, 0.f, 0.f};
+    if (v < o.v) {
+      g = sum4(a.sums + at * a.lds + v, a.splits, a.split_stride);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        g[i] = v + i < o.v ? __expf(g[i] - lse) - (v + i == y ? 1.f : 0.f) : 0.f;
+    }
+    store4<T>((T*)a.g + at * a.ldg + v, g, g_scale<T>(), 4, true);
+  }
 }
 
 // Joins the pairs of a row, a wave a row, for few rows with many pairs each.
@@ -434,9 +561,9 @@ __device__ __forceinline__ float row_loss(const JoinArgs& a, int j, int r, int p
 __global__ __launch_bounds__(256) void xent_join_wide(JoinArgs a) {
   const int j = blockIdx.y, lane = threadIdx.x & 63;
   const int r0 = blockIdx.x * 4 + (threadIdx.x >> 6);
-  double total = 0.0;
+  double total = 0.0, rows = 0.0;
   for (int r = r0; r < a.n; r += gridDim.x * 4) {
-    const int p = a.pos[(int64_t)j * a.n + r];
+    const int p = place_of(a, j, r);
     float m = NEG_INF, e = 0.f;
     if (p >= 0) {
       const float2* at = a.part + (int64_t)j * a.parts * a.cap + p;
@@ -448,11 +575,15 @@ __global__ __launch_bounds__(256) void xent_join_wide(JoinArgs a) {
 #pragma unroll
       for (int o = 32; o; o >>= 1) join(m, e, __shfl_xor(m, o), __shfl_xor(e, o));
     }
-    if (lane == 0) total += row_loss(a, j, r, p, m, e);
+    if (lane == 0) {
+      total += row_loss(a, j, r, p, m, e, p >= 0 ? a.plog[(int64_t)j * a.cap + p] : 0.f);
+      rows += p >= 0;
+    }
   }
   if (!a.loss) return;
   total = block_sum(total);
-  if (threadIdx.x == 0) a.loss[j] = (float)(total / max(a.cnt[j], 1));
+  rows = block_sum(rows);
+  if (threadIdx.x == 0) a.loss[j] = (float)(total / fmax(rows, 1.0));
 }
 
 // The same with eight threads a row and neighbouring rows in neighbouring
@@ -461,7 +592,7 @@ __global__ __launch_bounds__(256) void xent_join_rows(JoinArgs a) {
   const int j = blockIdx.y, x = threadIdx.x % 32, s = threadIdx.x / 32;
   const int r = blockIdx.x * 32 + x;
   __shared__ float2 pairs[8][32];
-  const int p = r < a.n ? a.pos[(int64_t)j * a.n + r] : -1;
+  const int p = r < a.n ? place_of(a, j, r) : -1;
   float m = NEG_INF, e = 0.f;
   if (p >= 0) {
     const float2* at = a.part + (int64_t)j * a.parts * a.cap + p;
@@ -475,18 +606,21 @@ __global__ __launch_bounds__(256) void xent_join_rows(JoinArgs a) {
   __syncthreads();
   if (s || r >= a.n) return;
   for (int i = 1; i < 8; ++i) join(m, e, pairs[i][x].x, pairs[i][x].y);
-  row_loss(a, j, r, p, m, e);
+  row_loss(a, j, r, p, m, e, p >= 0 ? a.plog[(int64_t)j * a.cap + p] : 0.f);
 }
 
 // A learner's mean loss over its counted rows (0 if none counts), in fp64.
-__global__ __launch_bounds__(256) void xent_mean(const float* rloss, const int* cnt, int n,
-                                                 float* loss) {
+__global__ __launch_bounds__(256) void xent_mean(JoinArgs a, float* loss) {
   const int j = blockIdx.x;
-  double t = 0.0;
+  double t = 0.0, rows = 0.0;
 #pragma unroll 4
-  for (int i = threadIdx.x; i < n; i += 256) t += rloss[(int64_t)j * n + i];
+  for (int i = threadIdx.x; i < a.n; i += 256) {
+    t += a.rloss[(int64_t)j * a.n + i];
+    rows += place_of(a, j, i) >= 0;
+  }
   t = block_sum(t);
-  if (threadIdx.x == 0) loss[j] = (float)(t / max(cnt[j], 1));
+  rows = block_sum(rows);
+  if (threadIdx.x == 0) loss[j] = (float)(t / fmax(rows, 1.0));
 }
 
 // --- gradients -------------------------------------------------------------------
@@ -536,26 +670,21 @@ __global__ __launch_bounds__(TL::THREADS, 2) void xent_dh_sums(DhArgs a) {
   });
 }
 
-// dh from the splits' sums; zero where the label is ignored.
+// dh from the splits' sums, four neighbouring columns a thread; zero where
+// the label is ignored.
 template <class T>
 __global__ __launch_bounds__(256) void xent_dh(const float* sums, int splits, int64_t split_stride,
                                                const int* pos, const int* cnt, int n, int d,
                                                int dp, int cap, float scale, T* dh) {
-  const int j = blockIdx.y, lane = threadIdx.x & 63;
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= n) return;
-  const int p = pos[(int64_t)j * n + r];
+  const int j = blockIdx.y, quads = (d + 3) / 4;
   const float f = scale / max(cnt[j], 1);
-  T* out = dh + ((int64_t)j * n + r) * d;
-  const float* in = sums + ((int64_t)j * cap + max(p, 0)) * dp;
-  // four neighbouring columns a lane: dp is a multiple of four
-  for (int x = lane * 4; x < d; x += 256) {
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < (int64_t)n * quads;
+       i += gridDim.x * 256ll) {
+    const int64_t r = i / quads;
+    const int x = (int)(i - r * quads) * 4, p = pos[(int64_t)j * n + r];
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (p >= 0) {
-#pragma unroll 4
-      for (int s = 0; s < splits; ++s) v += *(const f32x4*)(in + s * split_stride + x);
-    }
-    store4<T>(out + x, v, f, d - x, false);
+    if (p >= 0) v = sum4(sums + ((int64_t)j * cap + p) * dp + x, splits, split_stride);
+    store4<T>(dh + ((int64_t)j * n + r) * d + x, v, f, d - x, false);
   }
 }
 
@@ -569,6 +698,8 @@ struct DwArgs {
   void* dw;         // the piece's first row
   int64_t dstride;
   int vec;          // rows start on 4 elements
+  float* sums;      // [splits][k][vn][dp], or nullptr: write dw
+  int64_t split_stride;
 };
 
 // dW rows of the piece: P = h in col form (p = column), Q = g in col form
@@ -585,13 +716,33 @@ __global__ __launch_bounds__(TL::THREADS, 2) void xent_dw(DwArgs a) {
   const Operand<T> H{(const T*)a.hc + (int64_t)j * a.cap * a.dp, a.dp, a.dp, cnt};
   const Operand<T> G{(const T*)a.g + (int64_t)j * a.cap * a.ldg, a.ldg, a.ldg, cnt};
   typename TL::Acc acc;
-  TL::product(H, G, p0, q0, 0, cnt, lds, acc);
+  const int s = blockIdx.z, splits = gridDim.z;
+  const int span = (((cnt + splits - 1) / splits) + TL::BK - 1) / TL::BK * TL::BK;
+  TL::product(H, G, p0, q0, min(s * span, cnt), min((s + 1) * span, cnt), lds, acc);
   const float f = a.scale / max(cnt, 1);
   T* out = (T*)a.dw + j * a.dstride;
+  float* sums = a.sums ? a.sums + s * a.split_stride + (int64_t)j * a.vn * a.dp : nullptr;
   TL::for_each_quad(acc, [&](int p, int q, f32x4 v) {
     if (q0 + q >= a.vn || p0 + p >= a.d) return;
-    store4<T>(out + (int64_t)(q0 + q) * a.d + p0 + p, v, f, a.d - p0 - p, a.vec);
+    if (sums)
+      *(f32x4*)(sums + (int64_t)(q0 + q) * a.dp + p0 + p) = v;
+    else
+      store4<T>(out + (int64_t)(q0 + q) * a.d + p0 + p, v, f, a.d - p0 - p, a.vec);
   });
+}
+
+// dW from the splits' sums.
+template <class T>
+__global__ __launch_bounds__(256) void xent_dw_join(DwArgs a, int splits) {
+  const int j = blockIdx.y, quads = (a.d + 3) / 4;
+  const float f = a.scale / max(a.cnt[j], 1);
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < (int64_t)a.vn * quads;
+       i += gridDim.x * 256ll) {
+    const int64_t q = i / quads;
+    const int p = (int)(i - q * quads) * 4;
+    const f32x4 v = sum4(a.sums + ((int64_t)j * a.vn + q) * a.dp + p, splits, a.split_stride);
+    store4<T>((T*)a.dw + j * a.dstride + q * a.d + p, v, f, a.d - p, a.vec);
+  }
 }
 
 // --- launches ----------------------------------------------------------------------
@@ -603,43 +754,42 @@ using Mid = Tile<T, PC, QC, 128, 128, 2, 2>;
 template <class T, bool PC, bool QC>
 using Thin = Tile<T, PC, QC, 256, 32, 4, 1>;
 
-template <class T, bool BACKWARD>
-hipError_t launch_logits(const LogitArgs& a, int k, int n, hipStream_t s) {
-  constexpr int type = sizeof(T) == 4 ? LM_F32 : LM_BF16;
-  const int shape = shape_of(type, k, a.vn, n);
-  const dim3 grid((unsigned)tiles(a.vn, n, bp_of(shape), bq_of(shape)), k);
-  if constexpr (sizeof(T) == 2)
-    if (shape == BIG)
-      return launch_tile<Big<T, false, false>, xent_logits<Big<T, false, false>, BACKWARD>>(grid,
-                                                                                            s, a);
-  if (shape == MID)
-    return launch_tile<Mid<T, false, false>, xent_logits<Mid<T, false, false>, BACKWARD>>(grid, s,
-                                                                                          a);
-  return launch_tile<Thin<T, false, false>, xent_logits<Thin<T, false, false>, BACKWARD>>(grid, s,
-                                                                                          a);
+template <class T, int MODE>
+hipError_t launch_logits(const LogitArgs& a, Plan p, int k, int n, hipStream_t s) {
+  const dim3 grid((unsigned)tiles(a.vn, n, bp_of(p.shape), bq_of(p.shape)), k, p.splits);
+  if constexpr (sizeof(T) == 2 && MODE != SUMS)
+    if (p.shape == BIG)
+      return launch_tile<Big<T, false, false>, xent_logits<Big<T, false, false>, MODE>>(grid, s, a);
+  if (p.shape == MID)
+    return launch_tile<Mid<T, false, false>, xent_logits<Mid<T, false, false>, MODE>>(grid, s, a);
+  return launch_tile<Thin<T, false, false>, xent_logits<Thin<T, false, false>, MODE>>(grid, s, a);
 }
 
-// The parts of both passes that come first: the gathered rows and, where W's
-// own rows do not start on 16 bytes, its copy.
+// The parts of both passes that come first: the gathered rows (unless the
+// forward goes without) and, where W's own rows do not start on 16 bytes, its
+// copy.
 template <class T>
-hipError_t prepare(const XentArgs& a, const Layout& l, void* dh, LogitArgs& g, hipStream_t s) {
+hipError_t prepare(const XentArgs& a, const Layout& l, bool gather, void* dh, LogitArgs& g,
+                   hipStream_t s) {
   char* ws = (char*)a.ws;
   RowsArgs r{a.h, a.ldh, a.labels, a.ignore, a.n, a.d, l.dp, l.cap,
              (int*)(ws + l.cnt), (int*)(ws + l.pos), (int*)(ws + l.row), (int*)(ws + l.lab),
              ws + l.hc, dh};
-  const dim3 grid((a.n + ROWS_PER_BLOCK - 1) / ROWS_PER_BLOCK, a.k);
-  constexpr int E = 16 / sizeof(T);
-  if ((uintptr_t)a.h % 16 == 0 && a.ldh % E == 0 && a.d % E == 0)
-    klaunch(xent_rows<T, true>, grid, dim3(256), 0, s, r);
-  else
-    klaunch(xent_rows<T, false>, grid, dim3(256), 0, s, r);
-  if (hipError_t e = hipGetLastError()) return e;
+  if (gather) {
+    // a row a wave, unless that makes the counting dear
+    if (a.n <= 16384)
+      klaunch(xent_rows<T, 4>, dim3((a.n + 3) / 4, a.k), dim3(256), 0, s, r);
+    else
+      klaunch(xent_rows<T, 32>, dim3((a.n + 31) / 32, a.k), dim3(256), 0, s, r);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
   g.w = a.w;
   g.ldw = a.d;
   g.pstride = a.pstride;
   g.d = a.d;
   if (l.copy_w) {
-    klaunch(xent_copy_w<T>, dim3(std::min((a.v + 3) / 4, 4096), a.k), dim3(256), 0, s,
+    const int64_t blocks = ((int64_t)a.v * (l.dp / 8) + 255) / 256;
+    klaunch(xent_copy_w<T>, dim3((unsigned)std::min<int64_t>(blocks, 4096), a.k), dim3(256), 0, s,
             (const T*)a.w, a.pstride, a.v, a.d, l.dp, (T*)(ws + l.wc));
     if (hipError_t e = hipGetLastError()) return e;
     g.w = ws + l.wc;
@@ -649,14 +799,28 @@ hipError_t prepare(const XentArgs& a, const Layout& l, void* dh, LogitArgs& g, h
   }
   g.v0 = 0;
   g.vn = a.v;
-  g.hc = ws + l.hc;
-  g.dp = l.dp;
   g.cap = l.cap;
-  g.cnt = r.cnt;
-  g.lab = r.lab;
+  if (gather) {
+    g.hc = ws + l.hc;
+    g.dp = l.dp;
+    g.hstride = (int64_t)l.cap * l.dp;
+    g.cnt = r.cnt;
+    g.lab = r.lab;
+    g.ldlab = l.cap;
+  } else {
+    g.hc = a.h;
+    g.dp = a.ldh;
+    g.hstride = a.n * a.ldh;
+    g.lab = a.labels;
+    g.ldlab = a.n;
+  }
   g.row = r.row;
   g.n = a.n;
   g.lse = a.lse;
+  g.sums = (float*)(ws + l.lsum);
+  g.lds = (int)up(a.v, 256);
+  g.span = (int)up((g.d + l.logits.splits - 1) / l.logits.splits, 128 / sizeof(T));
+  g.split_stride = (int64_t)a.k * l.cap * g.lds;
   return hipSuccess;
 }
 
@@ -665,24 +829,39 @@ hipError_t forward(const XentArgs& a, hipStream_t s) {
   const Layout l = layout(a, false);
   char* ws = (char*)a.ws;
   LogitArgs g{};
-  if (hipError_t e = prepare<T>(a, l, nullptr, g, s)) return e;
+  // Few rows are not worth gathering where they can be read as they lie: a row
+  // that does not count fills its own column of the logits, which nobody reads.
+  constexpr int E = 16 / sizeof(T);
+  const bool gather = a.n > 32 || (uintptr_t)a.h % 16 || a.ldh % E || l.copy_w;
+  if (hipError_t e = prepare<T>(a, l, gather, nullptr, g, s)) return e;
   g.part = (float2*)(ws + l.part);
   g.plog = (float*)(ws + l.plog);
   g.parts = l.parts;
-  if (hipError_t e = launch_logits<T, false>(g, a.k, a.n, s)) return e;
   // up to 64 rows one workgroup takes all, and their mean; a wave a row fills
   // the card up to some thousands; the pairs of more rows are read best side
   // by side
-  const bool one = a.n <= 64;
-  JoinArgs o{g.cnt, (const int*)(ws + l.pos), g.lab, g.part, g.plog, l.parts, l.cap, a.n, a.v,
+  const bool summed = l.logits.splits > 1, wide = a.v > 1024;
+  const bool one = a.n <= 64 && !(summed && wide);
+  JoinArgs o{g.cnt, gather ? (const int*)(ws + l.pos) : nullptr, g.lab, a.ignore, g.ldlab, g.part, g.plog, l.parts, l.cap, a.n, a.v,
              a.lse, (float*)(ws + l.rloss), one ? a.loss : nullptr};
-  if (a.n < 2048)
-    klaunch(xent_join_wide, dim3(one ? 1 : (a.n + 3) / 4, a.k), dim3(256), 0, s, o);
-  else
-    klaunch(xent_join_rows, dim3((a.n + 31) / 32, a.k), dim3(256), 0, s, o);
+  const dim3 waves(one ? 1 : (a.n + 3) / 4, a.k);
+  if (summed) {
+    if (hipError_t e = launch_logits<T, SUMS>(g, l.logits, a.k, a.n, s)) return e;
+    SumArgs u{o, g.sums, l.logits.splits, g.lds, g.split_stride, nullptr, nullptr, nullptr, 0};
+    if (wide)
+      klaunch(xent_sums_loss<true>, dim3(a.n, a.k), dim3(256), 0, s, u);
+    else
+      klaunch(xent_sums_loss<false>, waves, dim3(256), 0, s, u);
+  } else {
+    if (hipError_t e = launch_logits<T, LOSS>(g, l.logits, a.k, a.n, s)) return e;
+    if (a.n < 2048)
+      klaunch(xent_join_wide, waves, dim3(256), 0, s, o);
+    else
+      klaunch(xent_join_rows, dim3((a.n + 31) / 32, a.k), dim3(256), 0, s, o);
+  }
   if (hipError_t e = hipGetLastError()) return e;
   if (one) return hipSuccess;
-  klaunch(xent_mean, dim3(a.k), dim3(256), 0, s, (const float*)o.rloss, g.cnt, a.n, a.loss);
+  klaunch(xent_mean, dim3(a.k), dim3(256), 0, s, o, a.loss);
   return hipGetLastError();
 }
 
@@ -692,8 +871,8 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
   char* ws = (char*)a.ws;
   LogitArgs g{};
   // one split: the last piece's product writes dh
-  void* direct = l.dhs.splits == 1 ? a.dh : nullptr;
-  if (hipError_t e = prepare<T>(a, l, direct, g, s)) return e;
+  void* direct = l.dh.splits == 1 ? a.dh : nullptr;
+  if (hipError_t e = prepare<T>(a, l, true, direct, g, s)) return e;
   g.g = ws + l.g;
   g.ldg = l.piece;
   constexpr int BK = 128 / (int)sizeof(T);
@@ -712,7 +891,7 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
   dh.cap = l.cap;
   dh.cnt = g.cnt;
   dh.row = g.row;
-  dh.sums = (float*)(ws + l.dh);
+  dh.sums = (float*)(ws + l.dhsum);
   dh.dp = l.dp;
   dh.split_stride = (int64_t)a.k * l.cap * l.dp;
   dh.vec = quads(a.dh, 0);
@@ -728,20 +907,46 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
   dw.scale = scale;
   dw.dstride = a.dstride;
   dw.vec = quads(a.dw, a.dstride);
+  dw.sums = l.dw.splits > 1 ? (float*)(ws + l.dwsum) : nullptr;
   const T* w = (const T*)g.w;
   for (int v0 = 0; v0 < a.v; v0 += l.piece) {
     const int vn = std::min(l.piece, a.v - v0);
     g.w = w + v0 * g.ldw;
     g.v0 = v0;
     g.vn = vn;
-    if (hipError_t e = launch_logits<T, true>(g, a.k, a.n, s)) return e;
+    if (l.logits.splits > 1) {
+      if (hipError_t e = launch_logits<T, SUMS>(g, l.logits, a.k, a.n, s)) return e;
+      SumArgs u{};
+      u.o.cnt = g.cnt;
+      u.o.lab = g.lab;
+      u.o.cap = l.cap;
+      u.o.n = a.n;
+      u.o.v = a.v;
+      u.sums = g.sums;
+      u.splits = l.logits.splits;
+      u.lds = g.lds;
+      u.split_stride = g.split_stride;
+      u.lse = a.lse;
+      u.row = g.row;
+      u.g = g.g;
+      u.ldg = g.ldg;
+      if (a.v > 1024)
+        klaunch(xent_sums_grad<T, 256>, dim3(a.n, a.k), dim3(256), 0, s, u);
+      else
+        klaunch(xent_sums_grad<T, 64>, dim3((a.n + 3) / 4, a.k), dim3(256), 0, s, u);
+      if (hipError_t e = hipGetLastError()) return e;
+    } else {
+      Plan p = plan_logits(a.type, a.k, a.n, g.d, vn);
+      p.splits = 1;
+      if (hipError_t e = launch_logits<T, GRAD>(g, p, a.k, a.n, s)) return e;
+    }
     dh.w = g.w;
     dh.vn = vn;
-    dh.span = (int)up((vn + l.dhs.splits - 1) / l.dhs.splits, BK);
+    dh.span = (int)up((vn + l.dh.splits - 1) / l.dh.splits, BK);
     dh.add = v0 > 0;
     dh.dh = v0 + vn == a.v ? direct : nullptr;
-    const int sd = l.dhs.shape;
-    const dim3 gd((unsigned)tiles(a.d, a.n, bp_of(sd), bq_of(sd)), a.k, l.dhs.splits);
+    const int sd = l.dh.shape;
+    const dim3 gd((unsigned)tiles(a.d, a.n, bp_of(sd), bq_of(sd)), a.k, l.dh.splits);
     hipError_t e = hipSuccess;
     if (sd == THIN)
       e = launch_tile<Thin<T, true, false>, xent_dh_sums<Thin<T, true, false>>>(gd, s, dh);
@@ -751,19 +956,27 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
       e = launch_tile<Big<T, true, false>, xent_dh_sums<Big<T, true, false>>>(gd, s, dh);
     if (e) return e;
     dw.vn = vn;
+    dw.split_stride = (int64_t)a.k * vn * l.dp;
     dw.dw = (T*)a.dw + (int64_t)v0 * a.d;
-    const int sw = big_or_mid(a.type, a.k * tiles(a.d, vn, 256, 256), a.k * tiles(a.d, vn, 128, 128));
-    const dim3 gw((unsigned)tiles(a.d, vn, bp_of(sw), bq_of(sw)), a.k);
-    if (sw == MID)
+    const Plan pw = l.dw.splits > 1 ? l.dw : plan(a.type, a.k, a.d, vn, 0, false, false);
+    const dim3 gw((unsigned)tiles(a.d, vn, bp_of(pw.shape), bq_of(pw.shape)), a.k, pw.splits);
+    if (pw.shape == MID)
       e = launch_tile<Mid<T, true, true>, xent_dw<Mid<T, true, true>>>(gw, s, dw);
     else if constexpr (sizeof(T) == 2)
       e = launch_tile<Big<T, true, true>, xent_dw<Big<T, true, true>>>(gw, s, dw);
     if (e) return e;
+    if (dw.sums) {
+      const int64_t blocks = ((int64_t)vn * ((a.d + 3) / 4) + 255) / 256;
+      klaunch(xent_dw_join<T>, dim3((unsigned)std::min<int64_t>(blocks, 2048), a.k), dim3(256), 0,
+              s, dw, l.dw.splits);
+      if (hipError_t e2 = hipGetLastError()) return e2;
+    }
   }
   if (direct) return hipSuccess;
-  klaunch(xent_dh<T>, dim3((a.n + 3) / 4, a.k), dim3(256), 0, s, (const float*)dh.sums, l.dhs.splits,
-          dh.split_stride, (const int*)(ws + l.pos), g.cnt, a.n, a.d, l.dp, l.cap, scale,
-          (T*)a.dh);
+  const int64_t blocks = ((int64_t)a.n * ((a.d + 3) / 4) + 255) / 256;
+  klaunch(xent_dh<T>, dim3((unsigned)std::min<int64_t>(blocks, 4096), a.k), dim3(256), 0, s,
+          (const float*)dh.sums, l.dh.splits, dh.split_stride, (const int*)(ws + l.pos), g.cnt,
+          a.n, a.d, l.dp, l.cap, scale, (T*)a.dh);
   return hipGetLastError();
 }
 
