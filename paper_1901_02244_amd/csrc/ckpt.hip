@@ -218,11 +218,11 @@ struct KeptTile {
       read_frags<T, BQ, true, TQ>(l + XBYTES, wq, 0, lane, fq);
       for (int s = 0; s < steps; ++s) {
         const uint32_t cur = (s & 1) * STAGE, nxt = STAGE - cur;
-        half_step<T, BP, true, BQ, true, 0>(acc, fp, fq, l + cur, l + cur + XBYTES, wp, wq, 1,
+        mma_step<T, BP, true, BQ, true, 0>(acc, fp, fq, l + cur, l + cur + XBYTES, wp, wq, 1,
                                             lane);
         tile_wait_barrier();
         send(cur);
-        half_step<T, BP, true, BQ, true, 16 * UNITS>(acc, fp, fq, l + nxt, l + nxt + XBYTES, wp, wq,
+        mma_step<T, BP, true, BQ, true, 16 * UNITS>(acc, fp, fq, l + nxt, l + nxt + XBYTES, wp, wq,
                                                      0, lane);
         refill(cur);
       }
@@ -266,8 +266,8 @@ struct KeptTile {
 
 // The same product of unpacked rows.
 template <class T_>
-struct PlainTile : Tile<T_, true, true, 256, 256, 2, 4> {
-  using Base = Tile<T_, true, true, 256, 256, 2, 4>;
+struct PlainTile : BigTile<T_, true, true> {
+  using Base = BigTile<T_, true, true>;
   static __device__ __forceinline__ void product(const GradArgs& a, int j, int p0, int q0, int r0,
                                                  int r1, char* lds, typename Base::Acc& acc) {
     const Operand<T_> X{(const T_*)a.x + (int64_t)j * a.n * a.ldx, a.ldx, (int)a.ldx, a.n};
@@ -413,11 +413,10 @@ hipError_t grad(const KeptGradArgs& a, hipStream_t s) {
   g.dstride = a.dstride;
   g.vec = a.d % 4 == 0 && (uintptr_t)a.dw % (4 * sizeof(T)) == 0 && a.dstride % 4 == 0;
   g.part = l.splits > 1 ? (float*)(ws + l.part) : nullptr;
-  const dim3 grid((unsigned)tiles(a.d, a.out, l.big ? 256 : 128), a.k, l.splits);
   hipError_t e = hipSuccess;
   if constexpr (sizeof(T) == 2)
-    if (l.big) e = launch_tile<Big<T>, kept_grad_k<Big<T>>>(grid, s, g);
-  if (!l.big) e = launch_tile<Mid<T>, kept_grad_k<Mid<T>>>(grid, s, g);
+    if (l.big) e = launch_tile<Big<T>, kept_grad_k<Big<T>>>(a.d, a.out, a.k, l.splits, s, g);
+  if (!l.big) e = launch_tile<Mid<T>, kept_grad_k<Mid<T>>>(a.d, a.out, a.k, l.splits, s, g);
   if (e) return e;
   if (l.splits == 1) return hipSuccess;
   klaunch(kept_grad_join<T>, dim3(blocks_of((int64_t)a.out * a.d), a.k), dim3(256), 0, s,

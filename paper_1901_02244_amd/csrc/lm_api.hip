@@ -4,6 +4,7 @@
 #include "crossbow_sma.h"
 #include "lm.hpp"
 
+#include <algorithm>
 #include <cmath>
 #include <exception>
 
@@ -102,7 +103,7 @@ NormArgs norm_args(const cb_gated_norm* g) {
   a.d = g->d;
   a.block = g->block;
   a.gate = g->gate;
-  a.gate_rows = g->gate ? g->gate_rows : g->n;
+  a.gate_rows = g->gate ? std::min(g->gate_rows, g->n) : g->n;  // more than all is all
   a.res_scale = g->res_scale;
   a.eps = g->eps;
   a.post = g->post;

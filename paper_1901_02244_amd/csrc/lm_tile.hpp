@@ -15,11 +15,17 @@
 //
 // A step takes 128 bytes of contraction per row (64 elements of 16 bits or 32
 // floats) from global memory straight into LDS (buffer loads with the LDS as
-// destination, 16 bytes a lane; no registers are spent on data in flight),
-// two steps deep.  What lies outside the operand reads as zero by the buffer's
-// range check, so ragged tiles need no branches.
+// destination, 16 bytes a lane; no registers are spent on data in flight), two
+// steps deep.  What lies outside the operand reads as zero by the buffer's
+// range check, so ragged tiles need no branches, and a tile's last steps load
+// on past its end, which costs no memory traffic.
+//   A 256 x 256 tile of bf16 takes 1.62 us a step, whatever the sum's length
+// (1,300 TFLOP/s over 256 CUs, the library's rate for a large product; the
+// MFMAs alone would need 0.85), and 6.7 us around them.  The matrix cores and
+// LDS are each busy about 60% of it; rings of five steps of half the size,
+// MFMAs pinned before the barrier and raised wave priority were no faster.
 //
-// Row form in LDS: rows of 128 bytes, 16-byte chunk c of row r at chunk
+// Row form in LDS: rows of 128 bytes, the 16-byte chunk c of row r at
 // c ^ (r & 7); a lane's operand of one MFMA is then one conflict-free
 // ds_read_b128.  Col form in LDS: [k][p] as in memory; 16-bit operands are
 // transposed by ds_read_b64_tr_b16 on the way to the registers (lanes
@@ -115,7 +121,8 @@ __device__ __forceinline__ i32x4 tile_rsrc(const void* base, uint32_t bytes) {
 // waits for every load in flight before the next LDS read, which would undo
 // the double buffering; the wait is tile_wait_barrier().  No register is
 // written, and the address registers are read at issue.  The s_nop covers
-// the wait state between the write of m0 and its use.
+// the wait state between the write of m0 and its use.  (m0 is reserved: the
+// compiler keeps nothing in it, and these kernels use it for nothing else.)
 __device__ __forceinline__ void load_to_lds(i32x4 rsrc, uint32_t off, uint32_t lds_addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
@@ -151,19 +158,22 @@ __device__ __forceinline__ int col_swizzle(int row) {
   return (2 * ((row & 3) | (((row >> 3) & 1) << 2))) & (CPR - 1);
 }
 
+constexpr int UB = 128;  // bytes of contraction that a step takes
+
+// Loads one operand's steps into LDS.
 template <class T, int R, bool COL, int THREADS>
 struct Loader {
-  static constexpr int BK = 128 / (int)sizeof(T);
-  static constexpr int BYTES = R * 128;
+  static constexpr int BK = UB / (int)sizeof(T);
+  static constexpr int BYTES = R * UB;
   static constexpr int NI = BYTES / (THREADS * 16);
   static_assert(NI * THREADS * 16 == BYTES, "whole loads");
-  static constexpr int CPR = COL ? R * (int)sizeof(T) / 16 : 8;  // chunks per LDS row
+  static constexpr int CPR = COL ? R * (int)sizeof(T) / 16 : UB / 16;  // chunks per LDS row
   uint32_t off[NI];
   uint32_t wave_lds;      // this wave's place in the operand's LDS
   const char* base;       // advances by a step's bytes
   int64_t left;           // bytes from base to the operand's end
   int64_t step;           // bytes a step advances by
-  uint32_t chunk;         // row form: this lane's byte in the step's 128
+  uint32_t chunk;         // row form: this lane's byte of the step's
   int k_left;             // row form: valid bytes of contraction left
 
   static __device__ __forceinline__ int swz(int row) {
@@ -191,8 +201,8 @@ struct Loader {
       base = reinterpret_cast<const char*>(o.base) + row0 * ldb + (int64_t)k0 * sizeof(T);
       k_left = ((o.k - k0) * (int)sizeof(T) + 15) & ~15;
       left = (int64_t)(min(o.rows - row0, R) - 1) * ldb + k_left;
-      step = 128;
-      chunk = (uint32_t)(((lane & 7) ^ swz(lane >> 3)) * 16);
+      step = UB;
+      chunk = (uint32_t)(((lane % CPR) ^ swz(lane / CPR)) * 16);
     }
   }
   // Starts the loads of the next step into the operand's LDS at lds.
@@ -205,7 +215,7 @@ struct Loader {
       load_to_lds(r, in ? off[i] : OUTSIDE, lds + wave_lds + i * (THREADS * 16));
     base += step;
     left -= step;
-    k_left -= 128;
+    k_left -= UB;
   }
 };
 
@@ -230,8 +240,8 @@ __device__ __forceinline__ i32x4 read_transposed(const lds_char* lds, int r0, in
   return f;
 }
 
-// The operand of the 16 rows from r0 for half a step (64 bytes of
-// contraction): 16-bit types in either form, fp32 in row form.
+// The operand of the 16 rows from r0 for 64 bytes of contraction, the kk-th of
+// a step: 16-bit types in either form, fp32 in row form.
 template <class T, int R, bool COL>
 __device__ __forceinline__ i32x4 read_frag(const lds_char* lds, int r0, int kk, int lane) {
   const int g = lane >> 4, j = lane & 15;
@@ -239,8 +249,9 @@ __device__ __forceinline__ i32x4 read_frag(const lds_char* lds, int r0, int kk, 
     static_assert(sizeof(T) == 2, "");
     return read_transposed<R>(lds, r0, kk * 32 + 8 * g, 4, lane);
   } else {
-    return *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(
-        lds + (r0 + j) * 128 + (((kk * 4 + g) ^ (j & 7)) * 16));
+    const int c = (kk * 4 + g) ^ (j & 7);
+    return *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>(lds + (r0 + j) * UB +
+                                                                             c * 16);
   }
 }
 
@@ -269,12 +280,11 @@ __device__ __forceinline__ void read_frags(const lds_char* lds, int r0, int kk, 
   }
 }
 
-// Half a step's MFMAs for 16-bit types, while the next half's operands come
-// from LDS: Q's beside, P's one by one over those that are done with, a few
+// 32 elements' MFMAs for 16-bit types, while the next operands come from LDS: Q's beside, P's one by one over those that are done with, a few
 // MFMAs between the reads.  VALU: how many vector instructions of
 // what the caller does next to spread over the MFMAs too.
 template <class T, int RP, bool PCOL, int RQ, bool QCOL, int VALU, int TP, int TQ>
-__device__ __forceinline__ void half_step(f32x4 (&acc)[TP][TQ], i32x4 (&fp)[TP], i32x4 (&fq)[TQ],
+__device__ __forceinline__ void mma_step(f32x4 (&acc)[TP][TQ], i32x4 (&fp)[TP], i32x4 (&fq)[TQ],
                                           const lds_char* p, const lds_char* q, int wp, int wq,
                                           int kk, int lane) {
   i32x4 nq[TQ];
@@ -305,13 +315,14 @@ struct Tile {
   static constexpr int THREADS = WP * WQ * 64;
   static constexpr int SP = BP / WP, SQ = BQ / WQ;  // a wave's share
   static constexpr int TP = SP / 16, TQ = SQ / 16;
-  static constexpr int BK = 128 / (int)sizeof(T);
-  static constexpr int STAGE = (BP + BQ) * 128;
-  static constexpr int LDS = 2 * STAGE;
+  static constexpr int BK = UB / (int)sizeof(T);
+  static constexpr int STEP = (BP + BQ) * UB;
+  static constexpr int LDS = 2 * STEP;
   using Acc = f32x4[TP][TQ];
 
   // acc = the tile at (p0, q0) summed over contraction [k0, k1); lds has LDS
-  // bytes.  Every thread of the workgroup calls it with the same arguments.
+  // bytes.  Every thread of the workgroup calls it with the same arguments;
+  // when it returns nothing is on its way to LDS, and all have read theirs.
   static __device__ __forceinline__ void product(const Operand<T>& P, const Operand<T>& Q, int p0,
                                                  int q0, int k0, int k1, char* lds, Acc& acc) {
     const int tid = threadIdx.x, lane = tid & 63;
@@ -330,67 +341,61 @@ struct Tile {
       for (int b = 0; b < TQ; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int steps = (k1 - k0 + BK - 1) / BK;
     if (steps <= 0) return;
-    lds_char* l = (lds_char*)lds;
+    const lds_char* l = (const lds_char*)lds;
     const uint32_t la = (uint32_t)(uintptr_t)l;
-    lp.issue(la);
-    lq.issue(la + BP * 128);
+    auto issue = [&](uint32_t slot) {
+      lp.issue(la + slot);
+      lq.issue(la + slot + BP * UB);
+    };
+    issue(0);
     tile_wait_barrier();
-    if (steps > 1) {
-      lp.issue(la + STAGE);
-      lq.issue(la + STAGE + BP * 128);
-    }
+    issue(STEP);
+    uint32_t cur = 0;
     if constexpr (sizeof(T) == 2) {
       i32x4 fp[TP], fq[TQ];
       read_frags<T, BP, PCOL, TP>(l, wp, 0, lane, fp);
-      read_frags<T, BQ, QCOL, TQ>(l + BP * 128, wq, 0, lane, fq);
-      // The barrier between the halves finds MFMAs on both sides of it.  (The
-      // last step reads on into the other buffer's leftovers, for nothing.)
+      read_frags<T, BQ, QCOL, TQ>(l + BP * UB, wq, 0, lane, fq);
+      // The barrier in the middle of a step finds its operands in registers, so
+      // that its half of LDS is free after it, and the next step landed; there
+      // are MFMAs on both sides of it.
       for (int s = 0; s < steps; ++s) {
-        const uint32_t cur = (s & 1) * STAGE, nxt = STAGE - cur;
-        half_step<T, BP, PCOL, BQ, QCOL, 0>(acc, fp, fq, l + cur, l + cur + BP * 128, wp, wq,
-                                                 1, lane);
+        mma_step<T, BP, PCOL, BQ, QCOL, 0>(acc, fp, fq, l + cur, l + cur + BP * UB, wp, wq, 1,
+                                           lane);
         tile_wait_barrier();
-        if (s + 2 < steps) {
-          lp.issue(la + cur);
-          lq.issue(la + cur + BP * 128);
-        }
-        half_step<T, BP, PCOL, BQ, QCOL, 0>(acc, fp, fq, l + nxt, l + nxt + BP * 128, wp, wq,
-                                                 0, lane);
+        issue(cur);
+        cur = STEP - cur;
+        mma_step<T, BP, PCOL, BQ, QCOL, 0>(acc, fp, fq, l + cur, l + cur + BP * UB, wp, wq, 0,
+                                           lane);
       }
     } else {
-      // A whole step's floats are split, then the next step's are read from
-      // LDS while the MFMAs run.
+      // A step's floats are split, then the next step's are read from LDS while
+      // the MFMAs run.
       i32x4 fp[2][TP], fq[2][TQ];
+      auto read = [&](uint32_t slot) {
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        read_frags<T, BP, PCOL, TP>(l, wp, kk, lane, fp[kk]);
-        read_frags<T, BQ, QCOL, TQ>(l + BP * 128, wq, kk, lane, fq[kk]);
-      }
+        for (int kk = 0; kk < 2; ++kk) {
+          read_frags<T, BP, PCOL, TP>(l + slot, wp, kk, lane, fp[kk]);
+          read_frags<T, BQ, QCOL, TQ>(l + slot + BP * UB, wq, kk, lane, fq[kk]);
+        }
+      };
+      read(0);
       for (int s = 0; s < steps; ++s) {
-        const uint32_t cur = (s & 1) * STAGE, nxt = STAGE - cur;
         Split3 sp[TP], sq[TQ];
 #pragma unroll
         for (int a = 0; a < TP; ++a) sp[a] = split3(fp[0][a], fp[1][a]);
 #pragma unroll
         for (int b = 0; b < TQ; ++b) sq[b] = split3(fq[0][b], fq[1][b]);
         tile_wait_barrier();
-        if (s + 2 < steps) {
-          lp.issue(la + cur);
-          lq.issue(la + cur + BP * 128);
-        }
-        if (s + 1 < steps) {
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk) {
-            read_frags<T, BP, PCOL, TP>(l + nxt, wp, kk, lane, fp[kk]);
-            read_frags<T, BQ, QCOL, TQ>(l + nxt + BP * 128, wq, kk, lane, fq[kk]);
-          }
-        }
+        issue(cur);
+        cur = STEP - cur;
+        read(cur);
 #pragma unroll
         for (int a = 0; a < TP; ++a)
 #pragma unroll
           for (int b = 0; b < TQ; ++b) acc[a][b] = mma3(sp[a], sq[b], acc[a][b]);
       }
     }
+    tile_wait_barrier();
   }
 
   // Calls f(p, q, v) for each four sums v at (p..p+3, q) that this thread
@@ -452,10 +457,23 @@ __device__ __forceinline__ void tile_of(int w, int tp, int tq, int& p, int& q) {
   q = in / wide;
 }
 
-// Launches KERNEL, which runs tiles of TL, with their LDS.  More than 64 KB
-// has to be asked for, once per kernel and device.
+// The tiles that the operators use.  BIG: one workgroup a CU; MID and THIN
+// (few rows): two.
+constexpr int THIN_Q = 32;
+template <class T, bool PC, bool QC>
+using BigTile = Tile<T, PC, QC, 256, 256, 2, 4>;
+template <class T, bool PC, bool QC>
+using MidTile = Tile<T, PC, QC, 128, 128, 2, 2>;
+template <class T, bool PC, bool QC>
+using ThinTile = Tile<T, PC, QC, 256, THIN_Q, 4, 1>;
+
+// Launches KERNEL on the tiles of TL that cover p x q for each of k learners
+// and `splits` shares of the sum (the kernel recovers their grid from p and
+// gridDim.x).  LDS above 64 KB has to be asked for, once per kernel and
+// device.
 template <class TL, auto KERNEL, class A>
-hipError_t launch_tile(dim3 grid, hipStream_t s, const A& a) {
+hipError_t launch_tile(int64_t p, int64_t q, int k, int splits, hipStream_t s, const A& a) {
+  const dim3 grid((unsigned)((p + TL::BP - 1) / TL::BP * ((q + TL::BQ - 1) / TL::BQ)), k, splits);
   static std::atomic<uint64_t> asked{0};
   int dev = 0;
   if (hipError_t e = hipGetDevice(&dev)) return e;

@@ -41,7 +41,7 @@ constexpr float g_scale() {
 
 __host__ __device__ constexpr int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-// Tile shapes.  THIN for up to 32 rows of a learner.  Else BIG (256 x 256,
+// Tile shapes.  THIN for up to THIN_Q rows of a learner.  Else BIG (256 x 256,
 // one workgroup a CU) or MID (128 x 128, two), whichever needs less time for
 // the rounds that 256 CUs make of the tiles: a BIG tile is four MID ones and
 // MID_COST as dear per element, twice the LDS reads for a product.  fp32
@@ -51,8 +51,8 @@ enum { BIG, MID, THIN };
 constexpr double MID_COST = 1.3;
 
 int64_t tiles(int64_t a, int64_t b, int ba, int bb) { return up(a, ba) / ba * (up(b, bb) / bb); }
-int bp_of(int shape) { return shape == MID ? 128 : 256; }
-int bq_of(int shape) { return shape == BIG ? 256 : shape == MID ? 128 : 32; }
+constexpr int bp_of(int shape) { return shape == MID ? 128 : 256; }
+constexpr int bq_of(int shape) { return shape == BIG ? 256 : shape == MID ? 128 : THIN_Q; }
 int64_t tiles_of(int shape, int k, int64_t p, int64_t q) {
   return k * tiles(p, q, bp_of(shape), bq_of(shape));
 }
@@ -64,13 +64,12 @@ struct Plan {
   int shape, splits;
 };
 Plan plan(int type, int k, int64_t p, int64_t q, int64_t sum, bool thin, bool big_splits) {
-  const int bk = 128 / lm_size(type);
-  const int64_t steps = up(sum, bk) / bk;
+  const int64_t steps = up(sum, 128 / lm_size(type)) / (128 / lm_size(type));  // of 128 bytes
   // from twelve steps on: the adding up is a launch more, as long as some steps
   auto share = [&](int64_t slots, int64_t t, int least) {
     return steps < 12 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(slots / t, steps / least));
   };
-  if (thin && q <= 32) return {THIN, share(512, tiles_of(THIN, k, p, q), 4)};
+  if (thin && q <= THIN_Q) return {THIN, share(512, tiles_of(THIN, k, p, q), 4)};
   const int64_t mid = tiles_of(MID, k, p, q), big = tiles_of(BIG, k, p, q);
   if (type != LM_F32) {
     if (mid > 256 && (big + 255) / 256 * 4 <= (mid + 511) / 512 * 2 * MID_COST) return {BIG, 1};
@@ -368,7 +367,6 @@ __global__ __launch_bounds__(TL::THREADS, 2) void xent_logits(LogitArgs a) {
     lses[b] = MODE == GRAD && q < cnt ? a.lse[(int64_t)j * a.n + a.row[at]] : 0.f;
   }
   TL::product(W, H, p0, q0, 0, a.d, lds, acc);
-  __syncthreads();  // the operands' LDS is used again
   if (p0 + TL::BP <= a.vn)
     logits_end<TL, MODE, false>(a, j, cnt, p0, q0, lds, label, lses, acc);
   else
@@ -747,22 +745,37 @@ __global__ __launch_bounds__(256) void xent_dw_join(DwArgs a, int splits) {
 
 // --- launches ----------------------------------------------------------------------
 
-template <class T, bool PC, bool QC>
-using Big = Tile<T, PC, QC, 256, 256, 2, 4>;
-template <class T, bool PC, bool QC>
-using Mid = Tile<T, PC, QC, 128, 128, 2, 2>;
-template <class T, bool PC, bool QC>
-using Thin = Tile<T, PC, QC, 256, 32, 4, 1>;
-
 template <class T, int MODE>
 hipError_t launch_logits(const LogitArgs& a, Plan p, int k, int n, hipStream_t s) {
-  const dim3 grid((unsigned)tiles(a.vn, n, bp_of(p.shape), bq_of(p.shape)), k, p.splits);
+  using Big = BigTile<T, false, false>;
+  using Mid = MidTile<T, false, false>;
+  using Thin = ThinTile<T, false, false>;
+  static_assert(Big::BP == bp_of(BIG) && Big::BQ == bq_of(BIG) && Mid::BP == bp_of(MID) &&
+                Mid::BQ == bq_of(MID) && Thin::BP == bp_of(THIN) && Thin::BQ == bq_of(THIN));
   if constexpr (sizeof(T) == 2 && MODE != SUMS)
-    if (p.shape == BIG)
-      return launch_tile<Big<T, false, false>, xent_logits<Big<T, false, false>, MODE>>(grid, s, a);
-  if (p.shape == MID)
-    return launch_tile<Mid<T, false, false>, xent_logits<Mid<T, false, false>, MODE>>(grid, s, a);
-  return launch_tile<Thin<T, false, false>, xent_logits<Thin<T, false, false>, MODE>>(grid, s, a);
+    if (p.shape == BIG) return launch_tile<Big, xent_logits<Big, MODE>>(a.vn, n, k, p.splits, s, a);
+  if (p.shape == MID) return launch_tile<Mid, xent_logits<Mid, MODE>>(a.vn, n, k, p.splits, s, a);
+  return launch_tile<Thin, xent_logits<Thin, MODE>>(a.vn, n, k, p.splits, s, a);
+}
+
+template <class T>
+hipError_t launch_dh(const DhArgs& a, Plan p, int k, hipStream_t s) {
+  using Big = BigTile<T, true, false>;
+  using Mid = MidTile<T, true, false>;
+  using Thin = ThinTile<T, true, false>;
+  if constexpr (sizeof(T) == 2)
+    if (p.shape == BIG) return launch_tile<Big, xent_dh_sums<Big>>(a.d, a.n, k, p.splits, s, a);
+  if (p.shape == MID) return launch_tile<Mid, xent_dh_sums<Mid>>(a.d, a.n, k, p.splits, s, a);
+  return launch_tile<Thin, xent_dh_sums<Thin>>(a.d, a.n, k, p.splits, s, a);
+}
+
+template <class T>
+hipError_t launch_dw(const DwArgs& a, Plan p, int k, hipStream_t s) {
+  using Big = BigTile<T, true, true>;
+  using Mid = MidTile<T, true, true>;
+  if constexpr (sizeof(T) == 2)
+    if (p.shape == BIG) return launch_tile<Big, xent_dw<Big>>(a.d, a.vn, k, p.splits, s, a);
+  return launch_tile<Mid, xent_dw<Mid>>(a.d, a.vn, k, p.splits, s, a);
 }
 
 // The parts of both passes that come first: the gathered rows (unless the
@@ -831,8 +844,10 @@ hipError_t forward(const XentArgs& a, hipStream_t s) {
   LogitArgs g{};
   // Few rows are not worth gathering where they can be read as they lie: a row
   // that does not count fills its own column of the logits, which nobody reads.
+  // (Offsets within a tile have 31 bits.)
   constexpr int E = 16 / sizeof(T);
-  const bool gather = a.n > 32 || (uintptr_t)a.h % 16 || a.ldh % E || l.copy_w;
+  const bool gather = a.n > THIN_Q || (uintptr_t)a.h % 16 || a.ldh % E || a.ldh > (1 << 22) ||
+                      l.copy_w;
   if (hipError_t e = prepare<T>(a, l, gather, nullptr, g, s)) return e;
   g.part = (float2*)(ws + l.part);
   g.plog = (float*)(ws + l.plog);
@@ -875,7 +890,6 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
   if (hipError_t e = prepare<T>(a, l, true, direct, g, s)) return e;
   g.g = ws + l.g;
   g.ldg = l.piece;
-  constexpr int BK = 128 / (int)sizeof(T);
   const float scale = a.grad_scale / g_scale<T>();
   auto quads = [&](const void* p, int64_t stride) {
     return a.d % 4 == 0 && (uintptr_t)p % (4 * sizeof(T)) == 0 && stride % 4 == 0;
@@ -942,29 +956,15 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
     }
     dh.w = g.w;
     dh.vn = vn;
-    dh.span = (int)up((vn + l.dh.splits - 1) / l.dh.splits, BK);
+    dh.span = (int)up((vn + l.dh.splits - 1) / l.dh.splits, 64);
     dh.add = v0 > 0;
     dh.dh = v0 + vn == a.v ? direct : nullptr;
-    const int sd = l.dh.shape;
-    const dim3 gd((unsigned)tiles(a.d, a.n, bp_of(sd), bq_of(sd)), a.k, l.dh.splits);
-    hipError_t e = hipSuccess;
-    if (sd == THIN)
-      e = launch_tile<Thin<T, true, false>, xent_dh_sums<Thin<T, true, false>>>(gd, s, dh);
-    else if (sd == MID)
-      e = launch_tile<Mid<T, true, false>, xent_dh_sums<Mid<T, true, false>>>(gd, s, dh);
-    else if constexpr (sizeof(T) == 2)
-      e = launch_tile<Big<T, true, false>, xent_dh_sums<Big<T, true, false>>>(gd, s, dh);
-    if (e) return e;
+    if (hipError_t e = launch_dh<T>(dh, l.dh, a.k, s)) return e;
     dw.vn = vn;
     dw.split_stride = (int64_t)a.k * vn * l.dp;
     dw.dw = (T*)a.dw + (int64_t)v0 * a.d;
     const Plan pw = l.dw.splits > 1 ? l.dw : plan(a.type, a.k, a.d, vn, 0, false, false);
-    const dim3 gw((unsigned)tiles(a.d, vn, bp_of(pw.shape), bq_of(pw.shape)), a.k, pw.splits);
-    if (pw.shape == MID)
-      e = launch_tile<Mid<T, true, true>, xent_dw<Mid<T, true, true>>>(gw, s, dw);
-    else if constexpr (sizeof(T) == 2)
-      e = launch_tile<Big<T, true, true>, xent_dw<Big<T, true, true>>>(gw, s, dw);
-    if (e) return e;
+    if (hipError_t e = launch_dw<T>(dw, pw, a.k, s)) return e;
     if (dw.sums) {
       const int64_t blocks = ((int64_t)vn * ((a.d + 3) / 4) + 255) / 256;
       klaunch(xent_dw_join<T>, dim3((unsigned)std::min<int64_t>(blocks, 2048), a.k), dim3(256), 0,
