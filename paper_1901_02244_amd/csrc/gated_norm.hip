@@ -50,12 +50,14 @@ Shape shape_of(int type, int d) {
 }
 constexpr int threads_of(int tpr) { return tpr < 128 ? 256 : tpr; }
 
-// 512 threads for every CU, the two waves a SIMD that the backward kernel's
-// registers let be resident, and at least four rows a worker where the rows
-// are few, so that the partial sums stay a small part of what is read.
-Split split_rows(int type, int k, int n, int d, int gate_rows) {
-  const int target = std::max(1, 256 * 512 / shape_of(type, d).tpr / k);
-  const int each = std::max(std::min(n, 4), (n + target - 1) / target);
+// Forward: 1024 threads for every CU.  Backward: 512, the two waves a SIMD
+// that its registers let be resident, and at least four rows a worker once
+// there are thousands, so that the partial sums stay a small part of what is
+// read.
+Split split_rows(int type, int k, int n, int d, int gate_rows, bool backward) {
+  const int target = std::max(1, 256 * (backward ? 512 : 1024) / shape_of(type, d).tpr / k);
+  const int least = backward && (int64_t)k * n > 1024 ? std::min(n, 4) : 1;
+  const int each = std::max(least, (n + target - 1) / target);
   Split s;
   if (gate_rows <= each) {
     s.span = (each + gate_rows - 1) / gate_rows * gate_rows;
@@ -413,17 +415,17 @@ hipError_t run(const Dev& v, bool backward, hipStream_t s) {
   return hipGetLastError();
 }
 
-Dev dev_of(const NormArgs& a) {
+Dev dev_of(const NormArgs& a, bool backward) {
   Dev v;
   v.a = a;
   if (!a.gate) v.a.gate_rows = a.n;
-  v.s = split_rows(a.type, a.k, a.n, a.d, v.a.gate_rows);
+  v.s = split_rows(a.type, a.k, a.n, a.d, v.a.gate_rows, backward);
   v.part = (float*)a.ws;
   return v;
 }
 
 hipError_t dispatch(const NormArgs& a, bool backward, hipStream_t s) {
-  const Dev v = dev_of(a);
+  const Dev v = dev_of(a, backward);
   return a.type == LM_F32 ? run<float>(v, backward, s)
          : a.type == LM_F16 ? run<_Float16>(v, backward, s)
                             : run<__bf16>(v, backward, s);
@@ -432,7 +434,7 @@ hipError_t dispatch(const NormArgs& a, bool backward, hipStream_t s) {
 }  // namespace
 
 size_t norm_ws_bytes(int type, int k, int n, int d, int gate_rows) {
-  return (size_t)k * split_rows(type, k, n, d, gate_rows).workers() * 3 * d * sizeof(float);
+  return (size_t)k * split_rows(type, k, n, d, gate_rows, true).workers() * 3 * d * sizeof(float);
 }
 hipError_t norm_fwd(const NormArgs& a, hipStream_t s) { return dispatch(a, false, s); }
 hipError_t norm_bwd(const NormArgs& a, hipStream_t s) { return dispatch(a, true, s); }

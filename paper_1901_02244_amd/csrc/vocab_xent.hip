@@ -556,11 +556,12 @@ __global__ __launch_bounds__(256) void xent_sums_grad(SumArgs a) {
 // Joins the pairs of a row, a wave a row, for few rows with many pairs each.
 // With a.loss one workgroup takes all rows of a learner, and their mean (0 if
 // none counts) in fp64.
-__global__ __launch_bounds__(256) void xent_join_wide(JoinArgs a) {
-  const int j = blockIdx.y, lane = threadIdx.x & 63;
-  const int r0 = blockIdx.x * 4 + (threadIdx.x >> 6);
+__global__ __launch_bounds__(1024) void xent_join_wide(JoinArgs a) {
+  const int j = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int waves = blockDim.x >> 6;
+  __shared__ double sums[16][2];
   double total = 0.0, rows = 0.0;
-  for (int r = r0; r < a.n; r += gridDim.x * 4) {
+  for (int r = blockIdx.x * waves + wave; r < a.n; r += gridDim.x * waves) {
     const int p = place_of(a, j, r);
     float m = NEG_INF, e = 0.f;
     if (p >= 0) {
@@ -579,9 +580,17 @@ __global__ __launch_bounds__(256) void xent_join_wide(JoinArgs a) {
     }
   }
   if (!a.loss) return;
-  total = block_sum(total);
-  rows = block_sum(rows);
-  if (threadIdx.x == 0) a.loss[j] = (float)(total / fmax(rows, 1.0));
+  if (lane == 0) {
+    sums[wave][0] = total;
+    sums[wave][1] = rows;
+  }
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int i = 1; i < waves; ++i) {
+    total += sums[i][0];
+    rows += sums[i][1];
+  }
+  a.loss[j] = (float)(total / fmax(rows, 1.0));
 }
 
 // The same with eight threads a row and neighbouring rows in neighbouring
@@ -870,7 +879,7 @@ hipError_t forward(const XentArgs& a, hipStream_t s) {
   } else {
     if (hipError_t e = launch_logits<T, LOSS>(g, l.logits, a.k, a.n, s)) return e;
     if (a.n < 2048)
-      klaunch(xent_join_wide, waves, dim3(256), 0, s, o);
+      klaunch(xent_join_wide, waves, dim3(one ? std::min((a.n + 3) / 4 * 256, 1024) : 256), 0, s, o);
     else
       klaunch(xent_join_rows, dim3((a.n + 31) / 32, a.k), dim3(256), 0, s, o);
   }
