@@ -89,6 +89,59 @@ def test_xent_ignored_rows_have_no_effect(t):
 
 
 @pytest.mark.parametrize("t", TYPES, ids=str)
+def test_xent_few_ignored_rows_read_in_place(t):
+    """Up to 32 rows the forward reads h where it lies, ignored rows and all."""
+    h, w, y = xent_inputs(2, 21, 64, 300, t)
+    y[0, ::2] = IGNORE
+    y[1] = IGNORE
+    h[y == IGNORE] = torch.nan
+    loss, lse, dh, dw = xent_check(h, w, y)
+    assert loss[1] == 0 and (dw[1] == 0).all()
+
+
+@pytest.mark.parametrize("t", TYPES, ids=str)
+def test_xent_shared_sums(t):
+    """Few tiles and long sums, which workgroups share: logits over many columns, dW over many rows,
+    dh over many words; rows for every kernel that adds them up."""
+    scale = 256.0 if t == F16 else 1.0
+    for size in ((1, 20, 1600, 40), (2, 70, 2056, 1100), (1, 1700, 48, 33), (1, 200, 1030, 700)):
+        xent_check(*xent_inputs(*size, t, pad=0.3), scale=scale)
+
+
+@pytest.mark.parametrize("t", [F16, BF16], ids=str)
+def test_xent_past_four_gib(t):
+    """600,000 words of 4096: W and dW of 4.9 GB each.  All words but the last 300 are zero, so their
+    logits are 0 and their rows of dW one and the same."""
+    v, d, n, m = 600000, 4096, 3, 300
+    gen = torch.Generator().manual_seed(9)
+    tail, h = rand(gen, m, d, std=0.05, t=t), rand(gen, 1, n, d, t=t)
+    w = torch.zeros(1, v, d, dtype=t, device="cuda")
+    w[0, v - m:] = tail.cuda()
+    y = torch.tensor([[v - 1, v - m, 5]], dtype=torch.int32)
+    loss, lse = cb.cb_vocab_xent_fwd(h.cuda(), w, y.cuda())
+    dh, dw = cb.cb_vocab_xent_bwd(h.cuda(), w, y.cuda(), lse, grad_scale=4096.0)
+    H, L = h[0].double(), h[0].double() @ tail.double().T
+    want = torch.log((v - m) + L.exp().sum(1))
+    # sums of 600,000 terms in fp32, tile by tile: 20 roundings deep at the most
+    assert ((lse[0].cpu().double() - want).abs() < 1e-5).all()
+    hit = torch.stack([L[0, m - 1], L[1, 0], torch.tensor(0.0).double()])
+    assert abs(loss[0].item() - (want - hit).mean().item()) < 1e-5
+    p = (L - want[:, None]).exp()
+    g = p.clone()
+    g[0, m - 1] -= 1
+    g[1, 0] -= 1
+    f, u = 4096.0 / n, ref.u(t)
+    got, exp = dw[0, v - m:].cpu().double(), f * g.T @ H
+    assert ((got - exp).abs() <= 3 * u * f * (g.abs().T @ H.abs()) + 1e-6).all()
+    same = f * torch.exp(-want)[:, None].T @ H  # a zero word's row
+    rest = dw[0, 6:v - m]
+    assert (rest == rest[0]).all()
+    assert ((rest[0].cpu().double() - same[0]).abs() <= 3 * u * f * (torch.exp(-want) @ H.abs()) + 1e-6).all()
+    got, exp = dh[0].cpu().double(), f * g @ tail.double()
+    assert ((got - exp).abs() <= 3 * u * f * (g.abs() @ tail.double().abs()) + 1e-5).all()
+
+
+@pytest.mark.parametrize("t", TYPES, ids=str)
 def test_xent_label_out_of_range(t):
     """As in cb_step: the learner's loss is NaN, the gradient has no one-hot term."""
     h, w, y = xent_inputs(2, 5, 24, 50, t)
@@ -298,6 +351,77 @@ def test_norm_keeps_its_output(size, t):
     k, n, d = size
     used = k * n * -(-d // 32) * 33
     assert torch.equal(kept.data[:used], cb.cb_ckpt_pack(y).data[:used])
+
+
+def test_norm_gradients_by_differences():
+    """Every gradient against central differences (in 64 bits) of <y, dy> + <x', dres>."""
+    i, dy, dres = norm_inputs(1, 5, 12, 2, F32, seed=8)
+    s, eps = 0.5, 2.0 ** -10
+    _, _, back = norm_check(i, dy, dres, 2, s=s, eps=eps)
+    X, O, G, P, Q = (i[name].double().clone() for name in ("x", "block", "gate", "post", "pre"))
+
+    def value():
+        xo = X[0] + s * G[0][torch.arange(5) // 2] * (P[0] * O[0] * ref.rms(O[0], eps))
+        return (Q[0] * xo * ref.rms(xo, eps) * dy[0].double()).sum() + (xo * dres[0].double()).sum()
+
+    step = 1e-5
+    for wrt, name in ((X, "dx"), (O, "dblock"), (G, "dgate"), (P, "dpost"), (Q, "dpre")):
+        flat, got = wrt.view(-1), back[name].double().cpu().view(-1)
+        for at in range(flat.numel()):
+            keep = flat[at].item()
+            flat[at] = keep + step
+            up = value()
+            flat[at] = keep - step
+            down = value()
+            flat[at] = keep
+            # fp32's rounding of sums of order ten, and a third derivative of order ten times step^2
+            assert abs((up - down) / (2 * step) - got[at]) < 2e-5, (name, at)
+
+
+def test_ckpt_wgrad_by_differences():
+    """dw against differences of <unpacked W^T, dy>, which is linear in W."""
+    gen = torch.Generator().manual_seed(6)
+    x, dy = rand(gen, 1, 9, 40), rand(gen, 1, 9, 6)
+    kept = cb.cb_ckpt_pack(x.cuda())
+    dw, X = cb.cb_ckpt_wgrad(kept, dy.cuda())[0].cpu(), cb.cb_ckpt_unpack(kept)[0].cpu().double()
+    w = rand(gen, 6, 40).double()
+
+    def value(w):
+        return ((X @ w.T) * dy[0].double()).sum()
+
+    for o, c in ((0, 0), (2, 17), (5, 39), (3, 31), (4, 32)):
+        e = torch.zeros_like(w)
+        e[o, c] = 0.5
+        assert abs(value(w + e) - value(w - e) - dw[o, c]) < 1e-5
+
+
+def test_norm_and_ckpt_past_four_gib():
+    """Rows past 2^32 bytes: every row is worth what it is worth in a small call."""
+    n, d, m = 300000, 8192, 40
+    gen = torch.Generator("cuda").manual_seed(3)
+    x = torch.randint(-100, 100, (1, n, d), generator=gen, device="cuda", dtype=torch.int8).to(BF16)
+    pre = torch.rand(1, d, generator=gen, device="cuda") + 0.5
+    tail = x[:, n - m:].clone()
+    _, y = cb.cb_gated_norm_fwd(x, pre=pre)
+    assert torch.equal(y[:, n - m:], cb.cb_gated_norm_fwd(tail, pre=pre)[1])
+    xo, y = cb.cb_gated_norm_fwd(x, block=x, pre=pre, post=pre, res_scale=0.5)
+    to, ty = cb.cb_gated_norm_fwd(tail, block=tail, pre=pre, post=pre, res_scale=0.5)
+    assert torch.equal(y[:, n - m:], ty) and torch.equal(xo[:, n - m:], to)
+    how = dict(pre=pre, post=pre, res_scale=0.5)
+    big = cb.cb_gated_norm_bwd(xo, y, block=x, **how)
+    small = cb.cb_gated_norm_bwd(to, ty, block=tail, **how)
+    assert torch.equal(big["dx"][:, n - m:], small["dx"])
+    assert torch.equal(big["dblock"][:, n - m:], small["dblock"])
+    del big, xo, y
+    kept = cb.cb_ckpt_pack(x)
+    back = cb.cb_ckpt_unpack(kept)
+    assert torch.equal(back[:, n - m:], cb.cb_ckpt_unpack(cb.cb_ckpt_pack(tail)))
+    del back
+    dy = torch.zeros(1, n, 24, dtype=BF16, device="cuda")
+    dy[:, n - m:] = 1  # only the last rows count
+    dw = cb.cb_ckpt_wgrad(kept, dy)
+    want = cb.cb_ckpt_unpack(cb.cb_ckpt_pack(tail)).float().sum(1)  # whole numbers: exact
+    assert torch.equal(dw[0], want.expand(24, d).to(BF16))
 
 
 def test_norm_in_place():
@@ -512,3 +636,51 @@ def test_workspace_of_the_caller():
     with pytest.raises(cb.CBError) as e:
         cb.cb_vocab_xent_bwd(h, w, y, want[1], workspace=ws[:need - 256])
     assert e.value.code == cb.CB_ENOMEM
+
+
+def test_package_refuses_on_the_gpu():
+    """Shapes, types and strides that do not fit are refused before anything runs."""
+    h, w, y = (v.cuda() for v in xent_inputs(2, 8, 16, 30, F32))
+    lse = torch.zeros(2, 8, device="cuda")
+    x, pre = torch.zeros(2, 8, 16, device="cuda"), torch.zeros(2, 16, device="cuda")
+    kept = cb.cb_ckpt_pack(x)
+    bad = [
+        lambda: cb.cb_vocab_xent_fwd(h, w[:, :, :8], y),
+        lambda: cb.cb_vocab_xent_fwd(h, w[:1], y),
+        lambda: cb.cb_vocab_xent_fwd(h, w.half(), y),
+        lambda: cb.cb_vocab_xent_fwd(h, w, y.long()),
+        lambda: cb.cb_vocab_xent_fwd(h, w, y[:, :4]),
+        lambda: cb.cb_vocab_xent_fwd(h, w, y.cpu()),
+        lambda: cb.cb_vocab_xent_fwd(h.transpose(1, 2), w, y),
+        lambda: cb.cb_vocab_xent_fwd(h.expand(2, 8, 16)[:, ::2], w, y[:, :4]),  # learners not n rows apart
+        lambda: cb.cb_vocab_xent_fwd(h, w[:, ::2], y),
+        lambda: cb.cb_vocab_xent_fwd(h[:, :0], w, y[:, :0]),
+        lambda: cb.cb_vocab_xent_fwd(h, w, y, workspace=torch.zeros(1 << 20, device="cuda")),
+        lambda: cb.cb_vocab_xent_bwd(h, w, y, lse[:, :4]),
+        lambda: cb.cb_vocab_xent_bwd(h, w, y, lse, dw=torch.zeros(2, 30, 17, device="cuda")[:, :, :16]),
+        lambda: cb.cb_vocab_xent_bwd(h, w, y, lse, grad_scale=float("inf")),
+        lambda: cb.cb_gated_norm_fwd(x),
+        lambda: cb.cb_gated_norm_fwd(x[:, ::2], pre=pre),
+        lambda: cb.cb_gated_norm_fwd(x, pre=pre.half()),
+        lambda: cb.cb_gated_norm_fwd(x, pre=pre[:, :8]),
+        lambda: cb.cb_gated_norm_fwd(x, gate=x, pre=pre),
+        lambda: cb.cb_gated_norm_fwd(x, block=x, gate=x, gate_rows=2),
+        lambda: cb.cb_gated_norm_fwd(x, block=x, gate=x, gate_rows=0),
+        lambda: cb.cb_gated_norm_fwd(x, block=x, keep=True),
+        lambda: cb.cb_gated_norm_fwd(x, pre=pre, eps=0.0),
+        lambda: cb.cb_gated_norm_fwd(torch.zeros(1, 1, 16392, device="cuda"), pre=torch.zeros(1, 16392, device="cuda")),
+        lambda: cb.cb_gated_norm_bwd(x, pre=pre),
+        lambda: cb.cb_gated_norm_bwd(x, dy=x, block=x),
+        lambda: cb.cb_gated_norm_bwd(x, block=x),
+        lambda: cb.cb_gated_norm_bwd(x, dy=x, pre=pre, dpost=pre),
+        lambda: cb.cb_ckpt_pack(x[:, :, ::2]),
+        lambda: cb.cb_ckpt_unpack(cb.Kept(kept.data[:-64], kept.shape, kept.dtype)),
+        lambda: cb.cb_ckpt_unpack(cb.Kept(kept.data, (2, 8, 64), kept.dtype)),
+        lambda: cb.cb_ckpt_wgrad(kept, x.half()),
+        lambda: cb.cb_ckpt_wgrad(kept, x[:, :4]),
+        lambda: cb.cb_ckpt_wgrad(kept, x, dw=torch.zeros(2, 16, 15, device="cuda")),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises(cb.CBError) as e:
+            f()
+        assert e.value.code == cb.CB_EINVAL, i
