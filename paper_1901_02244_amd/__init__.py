@@ -79,7 +79,6 @@ class cb_gated_norm(ctypes.Structure):
 
 _lib = None
 _P = ctypes.c_void_p
-_ref = ctypes.byref
 
 
 def check_abi(L, path):
@@ -382,14 +381,18 @@ def _refuse(who, why):
     raise CBError(CB_EINVAL, f"{who}: {why}")
 
 
+_torch = None          # torch, and what every call needs of it, after the first call
 _type_codes = {}
+_F32 = _I32 = _U8 = None
 
 
 def _type_code(who, dtype):
     code = _type_codes.get(dtype)
     if code is None:
+        global _torch, _F32, _I32, _U8
         import torch
 
+        _torch, _F32, _I32, _U8 = torch, torch.float32, torch.int32, torch.uint8
         _type_codes.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
         code = _type_codes.get(dtype)
         if code is None:
@@ -419,65 +422,59 @@ def _outer(t):
     return t.stride(0) if t.shape[0] > 1 else t.numel()
 
 
-class _Call:
-    """The device and stream of one call: the device of `t` is current inside
-    `with`, and tensors that are made for another stream than torch's current one
-    are known there to the allocator."""
-
-    __slots__ = ("torch", "device", "index", "back", "given", "handle", "other")
-
-    def __init__(self, t, stream):
-        import torch
-
-        self.torch, self.device, self.index, self.given = torch, t.device, t.get_device(), stream
-
-    def __enter__(self):
-        cuda = self.torch.cuda
-        now = cuda.current_device()
-        self.back = now if now != self.index else -1
-        if self.back >= 0:
-            cuda.set_device(self.index)
-        self.handle = here = _current_stream(self.torch, self.index)
-        self.other = False
-        if self.given is not None:
-            self.handle = self.given.cuda_stream
-            self.other = self.handle != here
-        return self
-
-    def __exit__(self, *a):
-        if self.back >= 0:
-            self.torch.cuda.set_device(self.back)
-
-    def new(self, shape, dtype):
-        t = self.torch.empty(shape, dtype=dtype, device=self.device)
-        if self.other:
-            t.record_stream(self.given)
-        return t
-
-    def like(self, t):
-        n = self.torch.empty_like(t)
-        if self.other:
-            n.record_stream(self.given)
-        return n
-
-    def workspace(self, who, nbytes, given):
-        if given is None:
-            return self.new((max(nbytes, 1),), self.torch.uint8)
-        if given.dtype != self.torch.uint8 or not given.is_contiguous() \
-                or given.device != self.device:
-            _refuse(who, "the workspace is not a contiguous uint8 tensor on the inputs' device")
-        return given
-
-    def check(self, who, rc):
-        if rc:
-            raise CBError(rc, lib().cb_last_error(None).decode() or who)
+def _begin(t, stream):
+    """Makes the device of t current.  Returns the handle of the call's stream, that
+    stream where it is not torch's current one (the allocator has to know that new
+    tensors are used there) or None, and the device to return to or -1."""
+    cuda, index = _torch.cuda, t.get_device()
+    back = cuda.current_device()
+    if back != index:
+        cuda.set_device(index)
+    else:
+        back = -1
+    here = _current_stream(index)
+    if stream is None or stream.cuda_stream == here:
+        return here, None, back
+    return stream.cuda_stream, stream, back
 
 
-def _current_stream(torch, index):
+def _end(back):
+    if back >= 0:
+        _torch.cuda.set_device(back)
+
+
+def _current_stream(index):
     """The handle of torch's current stream of a device (the stream object itself
     takes microseconds to make)."""
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+    raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else _torch.cuda.current_stream(index).cuda_stream
+
+
+def _like(t, other):
+    n = _torch.empty_like(t)
+    if other is not None:
+        n.record_stream(other)
+    return n
+
+
+def _new(t, shape, dtype, other):
+    n = t.new_empty(shape, dtype=dtype)
+    if other is not None:
+        n.record_stream(other)
+    return n
+
+
+def _workspace(who, t, nbytes, given, other):
+    if given is None:
+        return _new(t, (nbytes or 1,), _U8, other)
+    if given.dtype != _U8 or not given.is_contiguous() or given.device != t.device:
+        _refuse(who, "the workspace is not a contiguous uint8 tensor on the inputs' device")
+    return given
+
+
+def _check(who, rc):
+    if rc:
+        raise CBError(rc, lib().cb_last_error(None).decode() or who)
 
 
 def _ptr(t):
@@ -485,8 +482,6 @@ def _ptr(t):
 
 
 def _xent(who, h, w, labels, ignore):
-    import torch
-
     code = _type_code(who, h.dtype)
     if h.dim() != 3 or w.dim() != 3:
         _refuse(who, "h is [k, n, d] and w [k, v, d]")
@@ -496,12 +491,15 @@ def _xent(who, h, w, labels, ignore):
         _refuse(who, "h is not on a GPU")
     if min(k, n, d, v) < 1:
         _refuse(who, "an empty dimension")
-    # rows of h may lie further apart than d, the same for all learners
-    ldh = h.stride(1) if n > 1 else h.stride(0) if k > 1 else d
-    if (d > 1 and h.stride(2) != 1) or ldh < d or (k > 1 and h.stride(0) != n * ldh):
-        _refuse(who, "h is not rows at one stride")
-    _need(who, "w", w, (k, v, d), h.dtype, h.device, outer=True)
-    _need(who, "labels", labels, (k, n), torch.int32, h.device)
+    ldh = d
+    if not h.is_contiguous():
+        # rows may lie further apart than d, the same for all learners
+        ldh = h.stride(1) if n > 1 else h.stride(0) if k > 1 else d
+        if (d > 1 and h.stride(2) != 1) or ldh < d or (k > 1 and h.stride(0) != n * ldh):
+            _refuse(who, "h is not rows at one stride")
+    dev = h.device
+    _need(who, "w", w, (k, v, d), h.dtype, dev, outer=True)
+    _need(who, "labels", labels, (k, n), _I32, dev)
     return cb_vocab_xent(code, k, n, d, v, ignore, h.data_ptr(), ldh, w.data_ptr(), _outer(w),
                          labels.data_ptr())
 
@@ -513,16 +511,18 @@ def cb_vocab_xent_fwd(h, w, labels, ignore=-100, workspace=None, stream=None):
 
     Returns (loss [k], lse [k, n]) in float32: each learner's mean over its counted
     rows (0 if none counts) and the rows' log-sum-exp, which the backward takes."""
-    import torch
-
     who = "cb_vocab_xent_fwd"
+    L = lib()
     x = _xent(who, h, w, labels, ignore)
-    with _Call(h, stream) as c:
-        loss, lse = c.new((x.k,), torch.float32), c.new((x.k, x.n), torch.float32)
-        nbytes = lib().cb_vocab_xent_workspace_bytes(_ref(x), 0)
-        ws = c.workspace(who, nbytes, workspace)
-        c.check(who, lib().cb_vocab_xent_fwd(_ref(x), loss.data_ptr(), lse.data_ptr(),
-                                             ws.data_ptr(), ws.numel(), c.handle))
+    r = ctypes.byref(x)
+    handle, other, back = _begin(h, stream)
+    try:
+        loss, lse = _new(h, (x.k,), _F32, other), _new(h, (x.k, x.n), _F32, other)
+        ws = _workspace(who, h, L.cb_vocab_xent_workspace_bytes(r, 0), workspace, other)
+        _check(who, L.cb_vocab_xent_fwd(r, loss.data_ptr(), lse.data_ptr(), ws.data_ptr(),
+                                        ws.numel(), handle))
+    finally:
+        _end(back)
     return loss, lse
 
 
@@ -531,44 +531,44 @@ def cb_vocab_xent_bwd(h, w, labels, lse, grad_scale=1.0, ignore=-100, dw=None, w
     """The gradients of grad_scale * loss of cb_vocab_xent_fwd, given its lse:
     (dh [k, n, d], dw [k, v, d]) in the inputs' type.  dw may be given, for
     instance as a view of a flat gradient vector; it is overwritten."""
-    import torch
-
     who = "cb_vocab_xent_bwd"
+    L = lib()
     x = _xent(who, h, w, labels, ignore)
-    _need(who, "lse", lse, (x.k, x.n), torch.float32, h.device)
-    with _Call(h, stream) as c:
-        dh = c.new((x.k, x.n, x.d), h.dtype)
+    r = ctypes.byref(x)
+    _need(who, "lse", lse, (x.k, x.n), _F32, h.device)
+    if dw is not None:
+        _need(who, "dw", dw, (x.k, x.v, x.d), h.dtype, h.device, outer=True)
+    handle, other, back = _begin(h, stream)
+    try:
+        dh = _new(h, (x.k, x.n, x.d), h.dtype, other)
         if dw is None:
-            dw = c.new((x.k, x.v, x.d), h.dtype)
-        else:
-            _need(who, "dw", dw, (x.k, x.v, x.d), h.dtype, h.device, outer=True)
-        nbytes = lib().cb_vocab_xent_workspace_bytes(_ref(x), 1)
-        ws = c.workspace(who, nbytes, workspace)
-        c.check(who, lib().cb_vocab_xent_bwd(_ref(x), lse.data_ptr(), grad_scale,
-                                             dh.data_ptr(), dw.data_ptr(), _outer(dw),
-                                             ws.data_ptr(), ws.numel(), c.handle))
+            dw = _new(h, (x.k, x.v, x.d), h.dtype, other)
+        ws = _workspace(who, h, L.cb_vocab_xent_workspace_bytes(r, 1), workspace, other)
+        _check(who, L.cb_vocab_xent_bwd(r, lse.data_ptr(), grad_scale, dh.data_ptr(),
+                                        dw.data_ptr(), _outer(dw), ws.data_ptr(), ws.numel(),
+                                        handle))
+    finally:
+        _end(back)
     return dh, dw
 
 
 def _norm(who, x, block, gate, gate_rows, res_scale, post, pre, eps):
-    import torch
-
-    code = _type_code(who, x.dtype)
-    if x.dim() != 3 or min(x.shape) < 1:
+    dtype, shape, dev = x.dtype, x.shape, x.device
+    code = _type_code(who, dtype)
+    if len(shape) != 3 or min(shape) < 1:
         _refuse(who, "x is [k, n, d], none of them 0")
-    k, n, d = x.shape
-    if not x.is_cuda:
-        _refuse(who, "x is not on a GPU")
-    _need(who, "x", x, x.shape, x.dtype, x.device)
+    k, n, d = shape
+    _need(who, "x", x, shape, dtype, dev)
     if block is not None:
-        _need(who, "block", block, x.shape, x.dtype, x.device)
+        _need(who, "block", block, shape, dtype, dev)
     if gate is not None:
         if not 1 <= gate_rows < 2**31:
             _refuse(who, "gate_rows is out of range")
-        _need(who, "gate", gate, (k, -(-n // gate_rows), d), x.dtype, x.device)
-    for name, t in (("post", post), ("pre", pre)):
-        if t is not None:
-            _need(who, name, t, (k, d), torch.float32, x.device, outer=True)
+        _need(who, "gate", gate, (k, -(-n // gate_rows), d), dtype, dev)
+    if post is not None:
+        _need(who, "post", post, (k, d), _F32, dev, outer=True)
+    if pre is not None:
+        _need(who, "pre", pre, (k, d), _F32, dev, outer=True)
     return cb_gated_norm(code, k, n, d, gate_rows if gate is not None else 1, res_scale, eps,
                          _ptr(block), _ptr(gate), _ptr(post), _ptr(pre),
                          _outer(post) if post is not None else 0,
@@ -588,15 +588,19 @@ def cb_gated_norm_fwd(x, block=None, gate=None, gate_rows=1, res_scale=1.0, post
     Returns (x_out, y), x_out being x without a block and y None without pre; with
     keep also y in 8 bits, as cb_ckpt_pack gives it."""
     who = "cb_gated_norm_fwd"
+    L = lib()
     g = _norm(who, x, block, gate, gate_rows, res_scale, post, pre, eps)
     if keep and pre is None:
         _refuse(who, "keep without pre")
-    with _Call(x, stream) as c:
-        xo = c.like(x) if block is not None else x
-        y = c.like(x) if pre is not None else None
-        kept = _new_kept(c, x) if keep else None
-        c.check(who, lib().cb_gated_norm_fwd(_ref(g), x.data_ptr(), xo.data_ptr(), _ptr(y),
-                                             _ptr(kept.data) if keep else None, c.handle))
+    handle, other, back = _begin(x, stream)
+    try:
+        xo = _like(x, other) if block is not None else x
+        y = _like(x, other) if pre is not None else None
+        kept = _new_kept(x, other) if keep else None
+        _check(who, L.cb_gated_norm_fwd(ctypes.byref(g), x.data_ptr(), xo.data_ptr(), _ptr(y),
+                                        kept.data.data_ptr() if keep else None, handle))
+    finally:
+        _end(back)
     return (xo, y, kept) if keep else (xo, y)
 
 
@@ -609,37 +613,42 @@ def cb_gated_norm_bwd(x_out, dy=None, dres=None, block=None, gate=None, gate_row
     Returns a dict: dx, and where their parts are there dblock, dgate (summed over
     the rows that share a gate row), dpost, dpre (float32 [k, d]; may be given as
     views of a flat gradient vector, and are overwritten)."""
-    import torch
-
     who = "cb_gated_norm_bwd"
+    L = lib()
     g = _norm(who, x_out, block, gate, gate_rows, res_scale, post, pre, eps)
+    r = ctypes.byref(g)
     if (dy is None) != (pre is None):
         _refuse(who, "dy goes with pre")
-    for name, t in (("dy", dy), ("dres", dres)):
-        if t is not None:
-            _need(who, name, t, x_out.shape, x_out.dtype, x_out.device)
+    if dy is not None:
+        _need(who, "dy", dy, x_out.shape, x_out.dtype, x_out.device)
+    if dres is not None:
+        _need(who, "dres", dres, x_out.shape, x_out.dtype, x_out.device)
     for name, t, of in (("dpost", dpost, post), ("dpre", dpre, pre)):
         if t is not None:
             if of is None:
                 _refuse(who, f"{name} without its gamma")
-            _need(who, name, t, (g.k, g.d), torch.float32, x_out.device, outer=True)
-    with _Call(x_out, stream) as c:
-        out = {"dx": c.like(x_out)}
+            _need(who, name, t, (g.k, g.d), _F32, x_out.device, outer=True)
+    handle, other, back = _begin(x_out, stream)
+    try:
+        dx = _like(x_out, other)
+        dblock = dgate = None
         if block is not None:
-            out["dblock"] = c.like(x_out)
+            dblock = _like(block, other)
         if gate is not None:
-            out["dgate"] = c.like(gate)
-        if post is not None:
-            out["dpost"] = dpost if dpost is not None else c.new((g.k, g.d), torch.float32)
-        if pre is not None:
-            out["dpre"] = dpre if dpre is not None else c.new((g.k, g.d), torch.float32)
-        ws = c.workspace(who, lib().cb_gated_norm_workspace_bytes(_ref(g)), workspace)
-        c.check(who, lib().cb_gated_norm_bwd(
-            _ref(g), x_out.data_ptr(), _ptr(dy), _ptr(dres), out["dx"].data_ptr(),
-            _ptr(out.get("dblock")), _ptr(out.get("dgate")), _ptr(out.get("dpost")),
-            _outer(out["dpost"]) if post is not None else 0, _ptr(out.get("dpre")),
-            _outer(out["dpre"]) if pre is not None else 0, ws.data_ptr(), ws.numel(), c.handle))
-    return out
+            dgate = _like(gate, other)
+        if post is not None and dpost is None:
+            dpost = _new(post, (g.k, g.d), _F32, other)
+        if pre is not None and dpre is None:
+            dpre = _new(pre, (g.k, g.d), _F32, other)
+        ws = _workspace(who, x_out, L.cb_gated_norm_workspace_bytes(r), workspace, other)
+        _check(who, L.cb_gated_norm_bwd(
+            r, x_out.data_ptr(), _ptr(dy), _ptr(dres), dx.data_ptr(), _ptr(dblock), _ptr(dgate),
+            _ptr(dpost), _outer(dpost) if dpost is not None else 0, _ptr(dpre),
+            _outer(dpre) if dpre is not None else 0, ws.data_ptr(), ws.numel(), handle))
+    finally:
+        _end(back)
+    out = {"dx": dx, "dblock": dblock, "dgate": dgate, "dpost": dpost, "dpre": dpre}
+    return {name: t for name, t in out.items() if t is not None}
 
 
 class Kept:
@@ -651,25 +660,20 @@ class Kept:
         self.data, self.shape, self.dtype = data, tuple(shape), dtype
 
 
-def _new_kept(c, x):
-    import torch
-
+def _new_kept(x, other):
     k, n, d = x.shape
     nbytes = lib().cb_ckpt_bytes(k * n, d)
     if nbytes == 0:
         _refuse("cb_ckpt_bytes", f"{tuple(x.shape)} is out of range")
-    return Kept(c.new((nbytes,), torch.uint8), x.shape, x.dtype)
+    return Kept(_new(x, (nbytes,), _U8, other), x.shape, x.dtype)
 
 
 def _check_kept(who, kept):
     """The type code of a Kept whose buffer is as long as its shape says."""
-    import torch
-
     code = _type_code(who, kept.dtype)
     need = lib().cb_ckpt_bytes(kept.shape[0] * kept.shape[1], kept.shape[2])
     b = kept.data
-    if not b.is_cuda or b.dtype != torch.uint8 or not b.is_contiguous() or need == 0 \
-            or b.numel() < need:
+    if not b.is_cuda or b.dtype != _U8 or not b.is_contiguous() or need == 0 or b.numel() < need:
         _refuse(who, f"the kept buffer is not {need} bytes on a GPU")
     return code
 
@@ -681,13 +685,14 @@ def cb_ckpt_pack(x, stream=None):
     code = _type_code(who, x.dtype)
     if x.dim() != 3 or min(x.shape) < 1:
         _refuse(who, "x is [k, n, d], none of them 0")
-    if not x.is_cuda:
-        _refuse(who, "x is not on a GPU")
     _need(who, "x", x, x.shape, x.dtype, x.device)
-    with _Call(x, stream) as c:
-        kept = _new_kept(c, x)
-        c.check(who, lib().cb_ckpt_pack(code, x.shape[0] * x.shape[1], x.shape[2], x.data_ptr(),
-                                        kept.data.data_ptr(), c.handle))
+    handle, other, back = _begin(x, stream)
+    try:
+        kept = _new_kept(x, other)
+        _check(who, lib().cb_ckpt_pack(code, x.shape[0] * x.shape[1], x.shape[2], x.data_ptr(),
+                                       kept.data.data_ptr(), handle))
+    finally:
+        _end(back)
     return kept
 
 
@@ -696,10 +701,13 @@ def cb_ckpt_unpack(kept, stream=None):
     who = "cb_ckpt_unpack"
     code = _check_kept(who, kept)
     k, n, d = kept.shape
-    with _Call(kept.data, stream) as c:
-        x = c.new(kept.shape, kept.dtype)
-        c.check(who, lib().cb_ckpt_unpack(code, k * n, d, kept.data.data_ptr(), x.data_ptr(),
-                                          c.handle))
+    handle, other, back = _begin(kept.data, stream)
+    try:
+        x = _new(kept.data, kept.shape, kept.dtype, other)
+        _check(who, lib().cb_ckpt_unpack(code, k * n, d, kept.data.data_ptr(), x.data_ptr(),
+                                         handle))
+    finally:
+        _end(back)
     return x
 
 
@@ -714,14 +722,17 @@ def cb_ckpt_wgrad(kept, dy, dw=None, workspace=None, stream=None):
         _refuse(who, "dy is [k, n, out]")
     out = dy.shape[2]
     _need(who, "dy", dy, (k, n, out), kept.dtype, kept.data.device)
-    with _Call(dy, stream) as c:
+    if dw is not None:
+        _need(who, "dw", dw, (k, out, d), kept.dtype, dy.device, outer=True)
+    L = lib()
+    handle, other, back = _begin(dy, stream)
+    try:
         if dw is None:
-            dw = c.new((k, out, d), kept.dtype)
-        else:
-            _need(who, "dw", dw, (k, out, d), kept.dtype, dy.device, outer=True)
-        ws = c.workspace(who, lib().cb_ckpt_wgrad_workspace_bytes(code, k, n, d, out,
-                                                                   dy.data_ptr()), workspace)
-        c.check(who, lib().cb_ckpt_wgrad(code, k, n, d, out, kept.data.data_ptr(), dy.data_ptr(),
-                                         dw.data_ptr(), _outer(dw), ws.data_ptr(), ws.numel(),
-                                         c.handle))
+            dw = _new(dy, (k, out, d), kept.dtype, other)
+        need = L.cb_ckpt_wgrad_workspace_bytes(code, k, n, d, out, dy.data_ptr())
+        ws = _workspace(who, dy, need, workspace, other)
+        _check(who, L.cb_ckpt_wgrad(code, k, n, d, out, kept.data.data_ptr(), dy.data_ptr(),
+                                    dw.data_ptr(), _outer(dw), ws.data_ptr(), ws.numel(), handle))
+    finally:
+        _end(back)
     return dw

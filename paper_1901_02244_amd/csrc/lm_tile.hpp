@@ -467,25 +467,31 @@ using MidTile = Tile<T, PC, QC, 128, 128, 2, 2>;
 template <class T, bool PC, bool QC>
 using ThinTile = Tile<T, PC, QC, 256, THIN_Q, 4, 1>;
 
-// Launches KERNEL on the tiles of TL that cover p x q for each of k learners
-// and `splits` shares of the sum (the kernel recovers their grid from p and
-// gridDim.x).  LDS above 64 KB has to be asked for, once per kernel and
-// device.
-template <class TL, auto KERNEL, class A>
-hipError_t launch_tile(int64_t p, int64_t q, int k, int splits, hipStream_t s, const A& a) {
-  const dim3 grid((unsigned)((p + TL::BP - 1) / TL::BP * ((q + TL::BQ - 1) / TL::BQ)), k, splits);
+// Launches KERNEL with LDS bytes of dynamic LDS.  More than 64 KB has to be
+// asked for, once per kernel and device.
+template <int LDS, auto KERNEL, class A>
+hipError_t launch_with_lds(dim3 grid, int threads, hipStream_t s, const A& a) {
   static std::atomic<uint64_t> asked{0};
   int dev = 0;
   if (hipError_t e = hipGetDevice(&dev)) return e;
   const uint64_t bit = dev < 64 ? 1ull << dev : 0;
   if (!(asked.load(std::memory_order_relaxed) & bit) || !bit) {
     if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS))
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, LDS))
       return e;
     asked.fetch_or(bit, std::memory_order_relaxed);
   }
-  klaunch(KERNEL, grid, dim3(TL::THREADS), TL::LDS, s, a);
+  klaunch(KERNEL, grid, dim3(threads), LDS, s, a);
   return hipGetLastError();
+}
+
+// Launches KERNEL on the tiles of TL that cover p x q for each of k learners
+// and `splits` shares of the sum (the kernel recovers their grid from p and
+// gridDim.x).
+template <class TL, auto KERNEL, class A>
+hipError_t launch_tile(int64_t p, int64_t q, int k, int splits, hipStream_t s, const A& a) {
+  const dim3 grid((unsigned)((p + TL::BP - 1) / TL::BP * ((q + TL::BQ - 1) / TL::BQ)), k, splits);
+  return launch_with_lds<TL::LDS, KERNEL>(grid, TL::THREADS, s, a);
 }
 
 }  // namespace cbk

@@ -648,15 +648,14 @@ struct DhArgs {
   float scale;
 };
 
-// dh: P = W in col form (p = column), Q = g in row form (q = row).
+// One tile, the w-th of the learner's, of split s of dh: P = W in col form
+// (p = column), Q = g in row form (q = row).
 template <class TL>
-__global__ __launch_bounds__(TL::THREADS, 2) void xent_dh_sums(DhArgs a) {
+__device__ __forceinline__ void dh_tile(const DhArgs& a, int j, int w, int s, char* lds) {
   using T = typename TL::T;
-  extern __shared__ __align__(16) char lds[];
-  const int j = blockIdx.y, cnt = a.cnt[j], s = blockIdx.z;
-  const int np = (a.d + TL::BP - 1) / TL::BP;
+  const int cnt = a.cnt[j];
   int tp, tq;
-  tile_of<8>(blockIdx.x, np, gridDim.x / np, tp, tq);
+  tile_of<8>(w, (a.d + TL::BP - 1) / TL::BP, (a.n + TL::BQ - 1) / TL::BQ, tp, tq);
   const int p0 = tp * TL::BP, q0 = tq * TL::BQ;
   if (q0 >= cnt) return;
   const Operand<T> W{(const T*)a.w + j * a.pstride, a.ldw, a.dw, a.vn};
@@ -709,21 +708,19 @@ struct DwArgs {
   int64_t split_stride;
 };
 
-// dW rows of the piece: P = h in col form (p = column), Q = g in col form
-// (q = word).
+// One tile of split s of the piece's rows of dW: P = h in col form (p =
+// column), Q = g in col form (q = word).
 template <class TL>
-__global__ __launch_bounds__(TL::THREADS, 2) void xent_dw(DwArgs a) {
+__device__ __forceinline__ void dw_tile(const DwArgs& a, int j, int w, int s, int splits,
+                                        char* lds) {
   using T = typename TL::T;
-  extern __shared__ __align__(16) char lds[];
-  const int j = blockIdx.y, cnt = a.cnt[j];
-  const int np = (a.d + TL::BP - 1) / TL::BP;
+  const int cnt = a.cnt[j];
   int tp, tq;
-  tile_of<8>(blockIdx.x, np, gridDim.x / np, tp, tq);
+  tile_of<8>(w, (a.d + TL::BP - 1) / TL::BP, (a.vn + TL::BQ - 1) / TL::BQ, tp, tq);
   const int p0 = tp * TL::BP, q0 = tq * TL::BQ;
   const Operand<T> H{(const T*)a.hc + (int64_t)j * a.cap * a.dp, a.dp, a.dp, cnt};
   const Operand<T> G{(const T*)a.g + (int64_t)j * a.cap * a.ldg, a.ldg, a.ldg, cnt};
   typename TL::Acc acc;
-  const int s = blockIdx.z, splits = gridDim.z;
   const int span = (((cnt + splits - 1) / splits) + TL::BK - 1) / TL::BK * TL::BK;
   TL::product(H, G, p0, q0, min(s * span, cnt), min((s + 1) * span, cnt), lds, acc);
   const float f = a.scale / max(cnt, 1);
@@ -736,6 +733,28 @@ __global__ __launch_bounds__(TL::THREADS, 2) void xent_dw(DwArgs a) {
     else
       store4<T>(out + (int64_t)(q0 + q) * a.d + p0 + p, v, f, a.d - p0 - p, a.vec);
   });
+}
+
+// Both gradients of a piece, which wait for the same g and not for each
+// other, in one launch: the CUs that one's last round leaves idle work on the
+// other.  hn = 0 or wn = 0 leaves one out.
+struct GradsArgs {
+  DhArgs h;
+  DwArgs w;
+  int hn, hs;  // tiles and splits of dh
+  int wn, ws;  // of dW
+};
+template <class TLH, class TLW>
+__global__ __launch_bounds__(TLH::THREADS, 2) void xent_grads(GradsArgs a) {
+  static_assert(TLH::THREADS == TLW::THREADS);
+  extern __shared__ __align__(16) char lds[];
+  // dW's tiles start at a multiple of the XCDs, so that tile_of finds them
+  // dealt out as it expects
+  const int hall = a.hn * a.hs, from = (hall + NXCD - 1) / NXCD * NXCD, x = blockIdx.x;
+  if (x < hall)
+    dh_tile<TLH>(a.h, blockIdx.y, x % a.hn, x / a.hn, lds);
+  else if (x >= from)
+    dw_tile<TLW>(a.w, blockIdx.y, (x - from) % a.wn, (x - from) / a.wn, a.ws, lds);
 }
 
 // dW from the splits' sums.
@@ -767,24 +786,42 @@ hipError_t launch_logits(const LogitArgs& a, Plan p, int k, int n, hipStream_t s
   return launch_tile<Thin, xent_logits<Thin, MODE>>(a.vn, n, k, p.splits, s, a);
 }
 
-template <class T>
-hipError_t launch_dh(const DhArgs& a, Plan p, int k, hipStream_t s) {
-  using Big = BigTile<T, true, false>;
-  using Mid = MidTile<T, true, false>;
-  using Thin = ThinTile<T, true, false>;
-  if constexpr (sizeof(T) == 2)
-    if (p.shape == BIG) return launch_tile<Big, xent_dh_sums<Big>>(a.d, a.n, k, p.splits, s, a);
-  if (p.shape == MID) return launch_tile<Mid, xent_dh_sums<Mid>>(a.d, a.n, k, p.splits, s, a);
-  return launch_tile<Thin, xent_dh_sums<Thin>>(a.d, a.n, k, p.splits, s, a);
+template <class TLH, class TLW>
+hipError_t launch_grads(GradsArgs a, Plan h, Plan w, int k, hipStream_t s) {
+  a.hn = (int)(h.splits ? tiles(a.h.d, a.h.n, TLH::BP, TLH::BQ) : 0);
+  a.wn = (int)(w.splits ? tiles(a.w.d, a.w.vn, TLW::BP, TLW::BQ) : 0);
+  a.hs = h.splits;
+  a.ws = w.splits;
+  const dim3 grid((unsigned)(up((int64_t)a.hn * a.hs, NXCD) + (int64_t)a.wn * a.ws), k);
+  return launch_with_lds<std::max(TLH::LDS, TLW::LDS), xent_grads<TLH, TLW>>(grid, TLH::THREADS, s,
+                                                                             a);
 }
 
+// Both gradients, in one launch where their tiles have as many threads.
 template <class T>
-hipError_t launch_dw(const DwArgs& a, Plan p, int k, hipStream_t s) {
-  using Big = BigTile<T, true, true>;
-  using Mid = MidTile<T, true, true>;
+hipError_t launch_grads(const DhArgs& h, Plan ph, const DwArgs& w, Plan pw, int k, hipStream_t s) {
+  using HBig = BigTile<T, true, false>;
+  using HMid = MidTile<T, true, false>;
+  using HThin = ThinTile<T, true, false>;
+  using WBig = BigTile<T, true, true>;
+  using WMid = MidTile<T, true, true>;
+  const Plan none{MID, 0};
+  GradsArgs a{h, w, 0, 0, 0, 0};
+  if (sizeof(T) == 2 && (ph.shape == BIG) != (pw.shape == BIG)) {
+    if constexpr (sizeof(T) == 2) {
+      if (ph.shape == BIG) {
+        if (hipError_t e = launch_grads<HBig, WBig>(a, ph, none, k, s)) return e;
+        return launch_grads<HMid, WMid>(a, none, pw, k, s);
+      }
+      if (hipError_t e = launch_grads<HBig, WBig>(a, none, pw, k, s)) return e;
+    }
+    return ph.shape == MID ? launch_grads<HMid, WMid>(a, ph, none, k, s)
+                           : launch_grads<HThin, WMid>(a, ph, none, k, s);
+  }
   if constexpr (sizeof(T) == 2)
-    if (p.shape == BIG) return launch_tile<Big, xent_dw<Big>>(a.d, a.vn, k, p.splits, s, a);
-  return launch_tile<Mid, xent_dw<Mid>>(a.d, a.vn, k, p.splits, s, a);
+    if (ph.shape == BIG) return launch_grads<HBig, WBig>(a, ph, pw, k, s);
+  return ph.shape == MID ? launch_grads<HMid, WMid>(a, ph, pw, k, s)
+                         : launch_grads<HThin, WMid>(a, ph, pw, k, s);
 }
 
 // The parts of both passes that come first: the gathered rows (unless the
@@ -968,12 +1005,11 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
     dh.span = (int)up((vn + l.dh.splits - 1) / l.dh.splits, 64);
     dh.add = v0 > 0;
     dh.dh = v0 + vn == a.v ? direct : nullptr;
-    if (hipError_t e = launch_dh<T>(dh, l.dh, a.k, s)) return e;
     dw.vn = vn;
     dw.split_stride = (int64_t)a.k * vn * l.dp;
     dw.dw = (T*)a.dw + (int64_t)v0 * a.d;
     const Plan pw = l.dw.splits > 1 ? l.dw : plan(a.type, a.k, a.d, vn, 0, false, false);
-    if (hipError_t e = launch_dw<T>(dw, pw, a.k, s)) return e;
+    if (hipError_t e = launch_grads<T>(dh, l.dh, dw, pw, a.k, s)) return e;
     if (dw.sums) {
       const int64_t blocks = ((int64_t)vn * ((a.d + 3) / 4) + 255) / 256;
       klaunch(xent_dw_join<T>, dim3((unsigned)std::min<int64_t>(blocks, 2048), a.k), dim3(256), 0,
