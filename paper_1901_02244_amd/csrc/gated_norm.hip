@@ -77,8 +77,11 @@ struct Dev {
   float* part;    // [k][workers][3][d] partial sums of dpre, dpost, dgate
 };
 
+// Sums over a worker's threads, to all of them.  A wave that is ahead may be
+// at its next call while another still reads the sums of this one, but not two
+// calls ahead, for the barrier between: two buffers in turn need no second one.
 template <int TPR, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[N]) {
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*both)[TPR / 64 + 1][3], int& turn) {
   constexpr int LANES = TPR < 64 ? TPR : 64;
 #pragma unroll
   for (int o = LANES / 2; o; o >>= 1)
@@ -86,6 +89,8 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[N]) {
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], o);
   if constexpr (TPR > 64) {
     const int wave = threadIdx.x >> 6;
+    turn ^= 1;
+    float(*lds)[3] = both[turn];
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
       for (int i = 0; i < N; ++i) lds[wave][i] = v[i];
@@ -155,7 +160,8 @@ template <class T, int TPR, int U, bool WHOLE>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_forward(Dev v) {
   const NormArgs& a = v.a;
   const int j = blockIdx.y, t = threadIdx.x % TPR, d = a.d;
-  __shared__ float lds[2][TPR / 64 + 1][1];
+  __shared__ float lds[2][TPR / 64 + 1][3];
+  int turn = 0;
   int worker, r0, r1;
   if (!my_rows<TPR>(v, worker, r0, r1)) return;
   Row<U> post, pre, gate;
@@ -183,7 +189,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_forward(Dev v) {
         for (int u = 0; u < U; ++u)
 #pragma unroll
           for (int i = 0; i < 8; ++i) s[0] += o[u][i] * o[u][i];
-        row_sums<TPR, 1>(s, lds[0]);
+        row_sums<TPR, 1>(s, lds, turn);
         ro = 1.f / sqrtf(s[0] * inv_d + a.eps);
       }
 #pragma unroll
@@ -200,7 +206,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_forward(Dev v) {
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[0] += x[u][i] * x[u][i];
-    row_sums<TPR, 1>(s, lds[1]);
+    row_sums<TPR, 1>(s, lds, turn);
     const float rx = 1.f / sqrtf(s[0] * inv_d + a.eps);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -234,7 +240,8 @@ template <class T, int TPR, int U, bool WHOLE>
 __global__ __launch_bounds__(threads_of(TPR), TPR > 512 ? 4 : 2) void norm_backward(Dev v) {
   const NormArgs& a = v.a;
   const int j = blockIdx.y, t = threadIdx.x % TPR, d = a.d;
-  __shared__ float lds_a[TPR / 64 + 1][3], lds_b[TPR / 64 + 1][1];
+  __shared__ float lds[2][TPR / 64 + 1][3];
+  int turn = 0;
   int worker, r0, r1;
   if (!my_rows<TPR>(v, worker, r0, r1)) return;
   Row<U> post, pre, gate, dpre, dpost, dgate;
@@ -286,7 +293,7 @@ __global__ __launch_bounds__(threads_of(TPR), TPR > 512 ? 4 : 2) void norm_backw
         s[1] += pre[u][i] * dy[u][i] * x[u][i];
         s[2] += o[u][i] * o[u][i];
       }
-    row_sums<TPR, 3>(s, lds_a);
+    row_sums<TPR, 3>(s, lds, turn);
     if (a.pre) {
       const float rx = 1.f / sqrtf(s[0] * inv_d + a.eps);
       const float m = s[1] * rx * inv_d;  // mean(a u)
@@ -318,7 +325,7 @@ __global__ __launch_bounds__(threads_of(TPR), TPR > 512 ? 4 : 2) void norm_backw
         q[0] += dx[u][i] * w;
       }
     if (a.post) {
-      row_sums<TPR, 1>(q, lds_b);
+      row_sums<TPR, 1>(q, lds, turn);
       q[0] *= inv_d;
 #pragma unroll
       for (int u = 0; u < U; ++u)

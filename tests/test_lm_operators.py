@@ -353,6 +353,29 @@ def test_norm_keeps_its_output(size, t):
     assert torch.equal(kept.data[:used], cb.cb_ckpt_pack(y).data[:used])
 
 
+@pytest.mark.parametrize("parts", [(0, 1, 0), (0, 1, 1), (1, 0, 1), (1, 1, 1)], ids=str)
+@pytest.mark.parametrize("size", [(4100, 1030), (2050, 4096), (1030, 9000)], ids=str)
+@pytest.mark.parametrize("t", TYPES, ids=str)
+def test_norm_rows_do_not_depend_on_the_call(t, size, parts):
+    """A row of a long call, where several waves walk many rows together, is what it is in a call of few rows."""
+    n, d = size
+    gen = torch.Generator("cuda").manual_seed(31)
+    post, pre, block = parts
+    x, o, dy, dres = (torch.randn(1, n, d, generator=gen, device="cuda").to(t) for _ in range(4))
+    gammas = {name: torch.rand(1, d, generator=gen, device="cuda") + 0.5 for name, there in (("post", post), ("pre", pre)) if there}
+
+    def both(rows):
+        how = dict(gammas, res_scale=0.5, **({"block": o[:, rows]} if block else {}))
+        xo, y = cb.cb_gated_norm_fwd(x[:, rows].contiguous(), **how)
+        back = cb.cb_gated_norm_bwd(xo, dy[:, rows].contiguous() if pre else None, dres=dres[:, rows].contiguous(), **how)
+        return [v for v in (xo if block else None, y if pre else None, back["dx"], back.get("dblock")) if v is not None]
+
+    whole = both(slice(0, n))
+    for at in range(0, n, 205):
+        for a, b in zip(whole, both(slice(at, at + 205))):
+            assert torch.equal(a[:, at:at + 205], b), at
+
+
 def test_norm_gradients_by_differences():
     """Every gradient against central differences (in 64 bits) of <y, dy> + <x', dres>."""
     i, dy, dres = norm_inputs(1, 5, 12, 2, F32, seed=8)
