@@ -23,6 +23,7 @@
 #include "kept.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace cbk {
 namespace {
@@ -107,6 +108,18 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*both)[TPR / 64 +
 
 template <int U>
 using Row = float[U][8];
+
+// Keeps x' an fp32 value until it is stored: the compiler may fold the
+// addition and the rounding to fp16 into one instruction with one rounding,
+// and the stored x' would then differ from its fp32 sum's in a last place (one
+// in some 25,000), by how the code around it was compiled.
+template <class T>
+__device__ __forceinline__ void stay_f32(float (&x)[8]) {
+  if constexpr (std::is_same_v<T, _Float16>) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm("" : "+v"(x[i]));
+  }
+}
 
 template <int TPR, int U, bool WHOLE, class T>
 __device__ __forceinline__ void load_row(const T* row, int t, int d, Row<U>& x) {
@@ -197,6 +210,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_forward(Dev v) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           x[u][i] += a.res_scale * gate[u][i] * (post[u][i] * (o[u][i] * ro));
+        stay_f32<T>(x[u]);
         store8<T, WHOLE>((T*)a.x_out + at, (u * TPR + t) * 8, d, x[u]);
       }
     }

@@ -376,6 +376,15 @@ def test_norm_rows_do_not_depend_on_the_call(t, size, parts):
             assert torch.equal(a[:, at:at + 205], b), at
 
 
+def test_norm_stream_is_the_rounded_sum():
+    """x' is the sum in fp32, rounded once more to fp16: the same however the instructions were chosen."""
+    gen = torch.Generator("cuda").manual_seed(32)
+    x, o, g = (torch.randn(1, 500, 1001, generator=gen, device="cuda").half() for _ in range(3))
+    xo, _ = cb.cb_gated_norm_fwd(x * 3, block=o, gate=g, gate_rows=1, res_scale=0.5, pre=torch.ones(1, 1001, device="cuda"))
+    # the product of two fp16 numbers is exact in fp32, so that its sum with x has one rounding
+    assert torch.equal(xo, ((x * 3).float() + 0.5 * (g.float() * o.float())).half())
+
+
 def test_norm_gradients_by_differences():
     """Every gradient against central differences (in 64 bits) of <y, dy> + <x', dres>."""
     i, dy, dres = norm_inputs(1, 5, 12, 2, F32, seed=8)
