@@ -68,9 +68,13 @@ __global__ __launch_bounds__(256) void kept_unpack_k(const char* q, const uint8_
 // Rows of dy that do not start on 16 bytes, copied to ones that do.
 template <class T>
 __global__ __launch_bounds__(256) void copy_rows(const T* x, int64_t rows, int d, int dp, T* y) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t r = blockIdx.x * 4ll + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4ll)
-    for (int c = lane; c < dp; c += 64) y[r * dp + c] = c < d ? x[r * d + c] : (T)0.f;
+  const int64_t units = rows * (dp / 8);
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < units; i += gridDim.x * 256ll) {
+    const int64_t r = i / (dp / 8);
+    const int c = (int)(i - r * (dp / 8)) * 8;
+    const Raw8<T> v = load_raw8<T, false>(x + r * d, c, d);
+    __builtin_memcpy(y + r * dp + c, v.w, sizeof(v.w));
+  }
 }
 
 struct GradArgs {
@@ -349,7 +353,7 @@ Layout layout(const KeptGradArgs& a) {
       (int)std::max<int64_t>(1, std::min<int64_t>((l.big ? 256 : 512) / t, steps / 4));
   l.span = (int)up((a.n + l.splits - 1) / l.splits, bk);
   l.splits = (a.n + l.span - 1) / l.span;
-  l.ldy = up(a.out, 16 / sz);
+  l.ldy = up(a.out, 8);
   l.copy_dy = a.out * sz % 16 || (uintptr_t)a.dy % 16;
   size_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -399,7 +403,7 @@ hipError_t grad(const KeptGradArgs& a, hipStream_t s) {
   g.dy = a.dy;
   g.ldy = a.out;
   if (l.copy_dy) {
-    klaunch(copy_rows<T>, dim3(blocks_of((int64_t)a.k * a.n * 64)), dim3(256), 0, s,
+    klaunch(copy_rows<T>, dim3(blocks_of((int64_t)a.k * a.n * (l.ldy / 8))), dim3(256), 0, s,
             (const T*)a.dy, (int64_t)a.k * a.n, a.out, (int)l.ldy, (T*)(ws + l.dy));
     if (hipError_t e = hipGetLastError()) return e;
     g.dy = ws + l.dy;

@@ -79,6 +79,11 @@ Plan plan(int type, int k, int64_t p, int64_t q, int64_t sum, bool thin, bool bi
   return {MID, share(512, mid, 4)};
 }
 
+// Above MANY rows of a learner, labels are counted and losses added by CHUNK
+// of them first; below, each workgroup that needs all of them reads them all,
+// which costs less than a launch.
+constexpr int MANY = 16384, CHUNK = 1024;
+
 // Places in the workspace, in bytes.
 struct Layout {
   int cap;       // rows of a learner, up to a multiple of 64
@@ -87,7 +92,8 @@ struct Layout {
   int parts;     // tiles of the vocabulary, each with a (max, sum) of a row
   Plan logits, dh, dw;
   bool copy_w;
-  size_t cnt, pos, row, lab, hc, wc, part, plog, rloss, g, lsum, dhsum, dwsum, total;
+  size_t cnt, chunks, pos, row, lab, hc, wc, part, plog, rloss, means, g, lsum, dhsum, dwsum,
+      total;
 };
 
 Plan plan_logits(int type, int k, int n, int d, int v) {
@@ -122,12 +128,13 @@ Layout layout(const XentArgs& a, bool backward) {
     return here;
   };
   l.cnt = take(k * 4);
+  l.chunks = n > MANY ? take(up(n, CHUNK) / CHUNK * k * 4) : 0;
   l.pos = take((int64_t)k * n * 4);
   l.row = take(rows * 4);
   l.lab = take(rows * 4);
   l.hc = take(rows * l.dp * sz);
   l.wc = l.copy_w ? take((int64_t)k * v * l.dp * sz) : 0;
-  l.part = l.plog = l.rloss = l.g = l.lsum = l.dhsum = l.dwsum = 0;
+  l.part = l.plog = l.rloss = l.means = l.g = l.lsum = l.dhsum = l.dwsum = 0;
   if (l.logits.splits > 1) l.lsum = take(l.logits.splits * rows * up(v, 256) * 4);
   if (backward) {
     l.g = take(rows * l.piece * sz);
@@ -138,6 +145,7 @@ Layout layout(const XentArgs& a, bool backward) {
     l.part = take((int64_t)l.parts * rows * 8);
     l.plog = take(rows * 4);
     l.rloss = take((int64_t)k * n * 4);
+    l.means = n > MANY ? take(up(n, CHUNK) / CHUNK * k * 16) : 0;
   }
   l.total = at;
   return l;
@@ -150,29 +158,55 @@ struct RowsArgs {
   int64_t ldh;
   const int32_t* labels;
   int ignore, n, d, dp, cap;
+  int* chunks;      // counted rows of each CHUNK, or nullptr
   int *cnt, *pos, *row, *lab;
   void* hc;
   void* dh;         // backward: rows that do not count get zeros, or nullptr
 };
 
+// Adds up one value of each of 256 threads; the sum is every thread's.
+template <class V>
+__device__ __forceinline__ V block_sum(V t) {
+  __shared__ V sum[4];
+#pragma unroll
+  for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sum[threadIdx.x >> 6] = t;
+  __syncthreads();
+  return sum[0] + sum[1] + sum[2] + sum[3];
+}
+
+__global__ __launch_bounds__(256) void xent_counts(RowsArgs a) {
+  const int j = blockIdx.y;
+  int c = 0;
+#pragma unroll
+  for (int i = threadIdx.x; i < CHUNK; i += 256) {
+    const int r = blockIdx.x * CHUNK + i;
+    c += r < a.n && a.labels[(int64_t)j * a.n + r] != a.ignore;
+  }
+  c = block_sum(c);
+  if (threadIdx.x == 0) a.chunks[(int64_t)j * gridDim.x + blockIdx.x] = c;
+}
+
 // Gathers the counted rows of a learner, in order: every workgroup counts the
-// labels before its own R rows (n/R workgroups reading up to n labels from L2
-// cost less than a second launch), then its four waves copy rows, padded with
+// labels before its own R rows, then its four waves copy rows, padded with
 // zeros to dp columns.  pos[r] is the gathered place of row r or -1, row[]
 // and lab[] its inverse and the labels there.
 template <class T, int R>
 __global__ __launch_bounds__(256) void xent_rows(RowsArgs a) {
   const int j = blockIdx.y, r0 = blockIdx.x * R, tid = threadIdx.x;
   const int32_t* lab = a.labels + (int64_t)j * a.n;
-  __shared__ int wave_sum[4], place[R];
-  int c = 0;
+  __shared__ int place[R];
+  int c = 0, from = 0;
+  if (a.chunks) {
+    const int done = r0 / CHUNK, per = (a.n + CHUNK - 1) / CHUNK;
 #pragma unroll 4
-  for (int i = tid; i < r0; i += 256) c += lab[i] != a.ignore;
-#pragma unroll
-  for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
-  if ((tid & 63) == 0) wave_sum[tid >> 6] = c;
-  __syncthreads();
-  const int before = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
+    for (int i = tid; i < done; i += 256) c += a.chunks[(int64_t)j * per + i];
+    from = done * CHUNK;
+  }
+#pragma unroll 4
+  for (int i = from + tid; i < r0; i += 256) c += lab[i] != a.ignore;
+  const int before = block_sum(c);
   if (tid < 64) {
     const int r = r0 + tid;
     const bool mine = tid < R && r < a.n;
@@ -419,20 +453,6 @@ struct JoinArgs {
   float* loss;      // one workgroup a learner: the mean too; else nullptr
 };
 
-// Adds up one fp64 value of each of 256 threads; the sum is thread 0's.
-__device__ __forceinline__ double block_sum(double t) {
-  __shared__ double sum[256];
-  const int tid = threadIdx.x;
-  __syncthreads();
-  sum[tid] = t;
-  __syncthreads();
-  for (int o = 128; o; o >>= 1) {
-    if (tid < o) sum[tid] += sum[tid + o];
-    __syncthreads();
-  }
-  return sum[0];
-}
-
 // The place of row r, or -1.
 __device__ __forceinline__ int place_of(const JoinArgs& a, int j, int r) {
   if (a.pos) return a.pos[(int64_t)j * a.n + r];
@@ -616,14 +636,34 @@ __global__ __launch_bounds__(256) void xent_join_rows(JoinArgs a) {
   row_loss(a, j, r, p, m, e, p >= 0 ? a.plog[(int64_t)j * a.cap + p] : 0.f);
 }
 
-// A learner's mean loss over its counted rows (0 if none counts), in fp64.
-__global__ __launch_bounds__(256) void xent_mean(JoinArgs a, float* loss) {
+// A learner's mean loss over its counted rows (0 if none counts), in fp64; of
+// many rows, the sum and count of each CHUNK first.
+__global__ __launch_bounds__(256) void xent_mean(JoinArgs a, int rows_each, double2* means,
+                                                 float* loss) {
+  const int j = blockIdx.y, r0 = blockIdx.x * rows_each, r1 = min(r0 + rows_each, a.n);
+  double t = 0.0, rows = 0.0;
+#pragma unroll 4
+  for (int i = r0 + threadIdx.x; i < r1; i += 256) {
+    t += a.rloss[(int64_t)j * a.n + i];
+    rows += place_of(a, j, i) >= 0;
+  }
+  t = block_sum(t);
+  rows = block_sum(rows);
+  if (threadIdx.x) return;
+  if (means)
+    means[(int64_t)j * gridDim.x + blockIdx.x] = {t, rows};
+  else
+    loss[j] = (float)(t / fmax(rows, 1.0));
+}
+__global__ __launch_bounds__(256) void xent_mean_join(const double2* means, int chunks,
+                                                      float* loss) {
   const int j = blockIdx.x;
   double t = 0.0, rows = 0.0;
 #pragma unroll 4
-  for (int i = threadIdx.x; i < a.n; i += 256) {
-    t += a.rloss[(int64_t)j * a.n + i];
-    rows += place_of(a, j, i) >= 0;
+  for (int i = threadIdx.x; i < chunks; i += 256) {
+    const double2 m = means[(int64_t)j * chunks + i];
+    t += m.x;
+    rows += m.y;
   }
   t = block_sum(t);
   rows = block_sum(rows);
@@ -832,14 +872,17 @@ hipError_t prepare(const XentArgs& a, const Layout& l, bool gather, void* dh, Lo
                    hipStream_t s) {
   char* ws = (char*)a.ws;
   RowsArgs r{a.h, a.ldh, a.labels, a.ignore, a.n, a.d, l.dp, l.cap,
-             (int*)(ws + l.cnt), (int*)(ws + l.pos), (int*)(ws + l.row), (int*)(ws + l.lab),
+             a.n > MANY ? (int*)(ws + l.chunks) : nullptr, (int*)(ws + l.cnt), (int*)(ws + l.pos), (int*)(ws + l.row), (int*)(ws + l.lab),
              ws + l.hc, dh};
   if (gather) {
     // a row a wave, unless that makes the counting dear
-    if (a.n <= 16384)
+    if (a.n <= MANY) {
       klaunch(xent_rows<T, 4>, dim3((a.n + 3) / 4, a.k), dim3(256), 0, s, r);
-    else
+    } else {
+      klaunch(xent_counts, dim3((a.n + CHUNK - 1) / CHUNK, a.k), dim3(256), 0, s, r);
+      if (hipError_t e = hipGetLastError()) return e;
       klaunch(xent_rows<T, 32>, dim3((a.n + 31) / 32, a.k), dim3(256), 0, s, r);
+    }
     if (hipError_t e = hipGetLastError()) return e;
   }
   g.w = a.w;
@@ -922,7 +965,15 @@ hipError_t forward(const XentArgs& a, hipStream_t s) {
   }
   if (hipError_t e = hipGetLastError()) return e;
   if (one) return hipSuccess;
-  klaunch(xent_mean, dim3(a.k), dim3(256), 0, s, o, a.loss);
+  if (a.n <= MANY) {
+    klaunch(xent_mean, dim3(1, a.k), dim3(256), 0, s, o, a.n, (double2*)nullptr, a.loss);
+    return hipGetLastError();
+  }
+  const int chunks = (a.n + CHUNK - 1) / CHUNK;
+  double2* means = (double2*)(ws + l.means);
+  klaunch(xent_mean, dim3(chunks, a.k), dim3(256), 0, s, o, CHUNK, means, (float*)nullptr);
+  if (hipError_t e = hipGetLastError()) return e;
+  klaunch(xent_mean_join, dim3(a.k), dim3(256), 0, s, (const double2*)means, chunks, a.loss);
   return hipGetLastError();
 }
 

@@ -150,6 +150,15 @@ def test_xent_label_out_of_range(t):
     assert torch.isnan(loss[0]) and torch.isfinite(loss[1])
 
 
+@pytest.mark.parametrize("t", TYPES, ids=str)
+@pytest.mark.parametrize("n", [16384, 16385, 40001])
+def test_xent_many_rows(n, t):
+    """Rows whose labels are counted, and losses added, in chunks; one learner counts none of its first chunks."""
+    h, w, y = xent_inputs(2, n, 24, 50, t, pad=0.4)
+    y[1, :3000] = IGNORE
+    xent_check(h, w, y)
+
+
 def test_xent_other_ignored_label():
     h, w, y = xent_inputs(1, 9, 16, 20, F32)
     y[0, 4] = 0
