@@ -16,8 +16,9 @@
 // the tiles take both operands straight to LDS.  Converting in every one of
 // the out/256 workgroups that read a tile of x costs more (8192 rows, 2048 x
 // 8192, bf16: 240 us against 216 us and 11 us for the unpacking).
-//   Where there are few tiles, workgroups share the rows and kept_grad_join
-// adds their sums in order.
+//   Where the tiles do not fill the CUs, or the last round of them leaves most
+// idle, that round's tiles are shared by workgroups that take some of the rows
+// each, and kept_grad_join adds their sums in order.
 #include "kept.hpp"
 #include "lm_tile.hpp"
 
@@ -85,11 +86,13 @@ struct GradArgs {
   int64_t dp;
   const void* dy;    // [k*n] rows, ldy apart
   int64_t ldy;
-  int n, d, out, span;
+  int n, d, out;
+  int full, tail;    // tiles that one workgroup takes, and that `splits` share
+  int splits, span;  // rows that each of these takes
   void* dw;
   int64_t dstride;
   int vec;
-  float* part;       // [splits][k][out][up4(d)] where the rows are split
+  float* part;       // [splits][tail] tiles of sums
 };
 
 template <class T_, int BP_, int BQ_, int WP_, int WQ_>
@@ -280,50 +283,67 @@ struct PlainTile : BigTile<T_, true, true> {
   }
 };
 
+// The learner and the place of tile x of all learners'.
+template <class TL>
+__device__ __forceinline__ void tile_at(const GradArgs& a, int x, int& j, int& p0, int& q0) {
+  const int np = (a.d + TL::BP - 1) / TL::BP, nq = (a.out + TL::BQ - 1) / TL::BQ;
+  int tp, tq;
+  j = x / (np * nq);
+  tile_of<8>(x - j * np * nq, np, nq, tp, tq);
+  p0 = tp * TL::BP;
+  q0 = tq * TL::BQ;
+}
+
 template <class TL>
 __global__ __launch_bounds__(TL::THREADS, 2) void kept_grad_k(GradArgs a) {
   using T = typename TL::T;
   extern __shared__ __align__(16) char lds[];
-  const int j = blockIdx.y, s = blockIdx.z;
-  const int np = (a.d + TL::BP - 1) / TL::BP;
-  int tp, tq;
-  tile_of<8>(blockIdx.x, np, gridDim.x / np, tp, tq);
-  const int p0 = tp * TL::BP, q0 = tq * TL::BQ;
+  int x = blockIdx.x, r0 = 0, r1 = a.n;
+  float* part = nullptr;
+  if (x >= a.full) {
+    const int s = (x - a.full) / a.tail, t = (x - a.full) % a.tail;
+    r0 = s * a.span;
+    r1 = min(r0 + a.span, a.n);
+    part = a.part + (int64_t)(x - a.full) * (TL::BP * TL::BQ);
+    x = a.full + t;
+  }
+  int j, p0, q0;
+  tile_at<TL>(a, x, j, p0, q0);
   typename TL::Acc acc;
-  TL::product(a, j, p0, q0, min(s * a.span, a.n), min((s + 1) * a.span, a.n), lds, acc);
-  const int64_t d4 = (a.d + 3) / 4 * 4;
-  float* part = a.part ? a.part + ((int64_t)s * gridDim.y + j) * a.out * d4 : nullptr;
+  TL::product(a, j, p0, q0, r0, r1, lds, acc);
   T* out = (T*)a.dw + j * a.dstride;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wp = (wave / TL::WQ) * TL::SP, wq = (wave % TL::WQ) * TL::SQ;
 #pragma unroll
   for (int y = 0; y < TL::TQ; ++y) {
-    const int q = q0 + wq + TL::Base::col_of(y, lane);
+    const int q = wq + TL::Base::col_of(y, lane);
 #pragma unroll
-    for (int x = 0; x < TL::TP; ++x) {
-      const int p = p0 + wp + x * 16 + 4 * (lane >> 4);
-      if (q >= a.out || p >= a.d) continue;
+    for (int t = 0; t < TL::TP; ++t) {
+      const int p = wp + t * 16 + 4 * (lane >> 4);
       if (part)
-        *(f32x4*)(part + q * d4 + p) = acc[x][y];
-      else
-        store4<T>(out + (int64_t)q * a.d + p, acc[x][y], 1.f, a.d - p, a.vec);
+        *(f32x4*)(part + q * TL::BP + p) = acc[t][y];
+      else if (q0 + q < a.out && p0 + p < a.d)
+        store4<T>(out + (int64_t)(q0 + q) * a.d + p0 + p, acc[t][y], 1.f, a.d - p0 - p, a.vec);
     }
   }
 }
 
-// The splits' sums in order.
-template <class T>
-__global__ __launch_bounds__(256) void kept_grad_join(const float* part, int splits, int out,
-                                                      int d, T* dw, int64_t dstride) {
-  const int j = blockIdx.y;
-  const int64_t d4 = (d + 3) / 4 * 4, all = (int64_t)gridDim.y * out * d4;
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < (int64_t)out * d; i += gridDim.x * 256ll) {
-    const int64_t q = i / d, p = i - q * d;
-    const float* at = part + ((int64_t)j * out + q) * d4 + p;
-    float v = 0.f;
-    for (int s = 0; s < splits; ++s) v += at[s * all];
-    dw[j * dstride + i] = from_f32<T>(v);
-  }
+// The shared tiles' sums in order: blockIdx.y is the tile, 1024 of its values
+// a workgroup.
+template <class TL>
+__global__ __launch_bounds__(256) void kept_grad_join(GradArgs a) {
+  using T = typename TL::T;
+  int j, p0, q0;
+  tile_at<TL>(a, a.full + blockIdx.y, j, p0, q0);
+  const int at = (blockIdx.x * 256 + threadIdx.x) * 4;
+  const int p = p0 + at % TL::BP, q = q0 + at / TL::BP;
+  if (p >= a.d || q >= a.out) return;
+  const float* from = a.part + (int64_t)blockIdx.y * (TL::BP * TL::BQ) + at;
+  f32x4 v = *(const f32x4*)from;
+#pragma unroll 4
+  for (int s = 1; s < a.splits; ++s)
+    v += *(const f32x4*)(from + (int64_t)s * a.tail * (TL::BP * TL::BQ));
+  store4<T>((T*)a.dw + j * a.dstride + (int64_t)q * a.d + p, v, 1.f, a.d - p, a.vec);
 }
 
 template <class T>
@@ -336,7 +356,7 @@ int64_t tiles(int64_t a, int64_t b, int t) { return up(a, t) / t * (up(b, t) / t
 
 struct Layout {
   bool big;
-  int splits, span;
+  int full, tail, splits, span;
   int64_t ldx, ldy;
   bool copy_dy;
   size_t x, dy, part, total;
@@ -348,11 +368,20 @@ Layout layout(const KeptGradArgs& a) {
   // tiles of 256 where they fill the 256 CUs; fp32, whose operands take more
   // registers, has tiles of 128 only
   l.big = a.type != LM_F32 && a.k * tiles(a.d, a.out, 256) >= 256;
-  const int64_t t = a.k * tiles(a.d, a.out, l.big ? 256 : 128), steps = up(a.n, bk) / bk;
-  l.splits =
-      (int)std::max<int64_t>(1, std::min<int64_t>((l.big ? 256 : 512) / t, steps / 4));
+  const int64_t side = l.big ? 256 : 128, slots = l.big ? 256 : 512;
+  const int64_t t = a.k * tiles(a.d, a.out, side), steps = up(a.n, bk) / bk;
+  // Behind full rounds the joining has to be worth it: from twelve steps on
+  // (bf16, 4096 x 4352, 16 tiles behind 256: 16,384 rows 567 us against 831 in
+  // two rounds, 1100 rows 71 against 81, 800 rows 59 against 65; 2048 x
+  // 11,008, 88 behind 256, 700 rows: 61 against 58).
+  const int64_t full = t / slots * slots, tail = t - full;
+  l.splits = 1;
+  if (tail && (!full || steps >= 12))
+    l.splits = (int)std::max<int64_t>(1, std::min(slots / tail, steps / 4));
   l.span = (int)up((a.n + l.splits - 1) / l.splits, bk);
   l.splits = (a.n + l.span - 1) / l.span;
+  l.full = (int)(l.splits > 1 ? full : t);
+  l.tail = (int)(t - l.full);
   l.ldy = up(a.out, 8);
   l.copy_dy = a.out * sz % 16 || (uintptr_t)a.dy % 16;
   size_t at = 0;
@@ -363,7 +392,7 @@ Layout layout(const KeptGradArgs& a) {
   };
   l.ldx = up(a.d, 8);
   l.x = l.big ? take((int64_t)a.k * a.n * l.ldx * sz) : 0;
-  l.part = l.splits > 1 ? take((int64_t)l.splits * a.k * a.out * up(a.d, 4) * 4) : 0;
+  l.part = l.tail ? take(l.splits * l.tail * side * side * 4) : 0;
   l.dy = l.copy_dy ? take((int64_t)a.k * a.n * l.ldy * sz) : 0;
   l.total = std::max<size_t>(at, 256);
   return l;
@@ -388,8 +417,19 @@ hipError_t pack(int64_t rows, int d, const void* x, void* kept, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <class TL>
+hipError_t launch_grad(const GradArgs& g, hipStream_t s) {
+  const dim3 grid(g.full + g.tail * g.splits);
+  if (hipError_t e = launch_with_lds<TL::LDS, kept_grad_k<TL>>(grid, TL::THREADS, s, g)) return e;
+  if (!g.tail) return hipSuccess;
+  klaunch(kept_grad_join<TL>, dim3(TL::BP * TL::BQ / 1024, g.tail), dim3(256), 0, s, g);
+  return hipGetLastError();
+}
+
 template <class T>
 hipError_t grad(const KeptGradArgs& a, hipStream_t s) {
+  static_assert(Big<_Float16>::BP == 256 && Big<_Float16>::BQ == 256 && Mid<T>::BP == 128 &&
+                Mid<T>::BQ == 128, "as layout() counts them");
   const Layout l = layout(a);
   char* ws = (char*)a.ws;
   GradArgs g;
@@ -412,20 +452,17 @@ hipError_t grad(const KeptGradArgs& a, hipStream_t s) {
   g.n = a.n;
   g.d = a.d;
   g.out = a.out;
+  g.full = l.full;
+  g.tail = l.tail;
+  g.splits = l.splits;
   g.span = l.span;
   g.dw = a.dw;
   g.dstride = a.dstride;
   g.vec = a.d % 4 == 0 && (uintptr_t)a.dw % (4 * sizeof(T)) == 0 && a.dstride % 4 == 0;
-  g.part = l.splits > 1 ? (float*)(ws + l.part) : nullptr;
-  hipError_t e = hipSuccess;
+  g.part = (float*)(ws + l.part);
   if constexpr (sizeof(T) == 2)
-    if (l.big) e = launch_tile<Big<T>, kept_grad_k<Big<T>>>(a.d, a.out, a.k, l.splits, s, g);
-  if (!l.big) e = launch_tile<Mid<T>, kept_grad_k<Mid<T>>>(a.d, a.out, a.k, l.splits, s, g);
-  if (e) return e;
-  if (l.splits == 1) return hipSuccess;
-  klaunch(kept_grad_join<T>, dim3(blocks_of((int64_t)a.out * a.d), a.k), dim3(256), 0, s,
-          (const float*)g.part, l.splits, a.out, a.d, (T*)a.dw, a.dstride);
-  return hipGetLastError();
+    if (l.big) return launch_grad<Big<T>>(g, s);
+  return launch_grad<Mid<T>>(g, s);
 }
 
 }  // namespace

@@ -561,6 +561,21 @@ def test_ckpt_wgrad_big_tiles(t):
 
 
 @pytest.mark.parametrize("t", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(3, 4110, 1500, 1890), (2, 4110, 2790, 3080)], ids=str)
+def test_ckpt_wgrad_few_tiles_behind_many(size, t):
+    """A last round of tiles whose rows are shared, of learners that start inside a round."""
+    k, n, d, out = size
+    gen = torch.Generator("cuda").manual_seed(5)
+    x, dy = (torch.randn(k, n, w, generator=gen, device="cuda").to(t) for w in (d, out))
+    kept = cb.cb_ckpt_pack(x)
+    dw = cb.cb_ckpt_wgrad(kept, dy)
+    values = cb.cb_ckpt_unpack(kept)
+    for j in range(k):
+        want, bound = ref.wgrad(values[j], dy[j])["dw"]
+        close(f"dw[{j}]", dw[j], (want.cpu(), bound.cpu()))
+
+
+@pytest.mark.parametrize("t", TYPES, ids=str)
 def test_ckpt_wgrad_of_nan(t):
     """A group of NaNs spoils its own 32 columns of dw and no others."""
     gen = torch.Generator().manual_seed(4)
