@@ -777,10 +777,12 @@ __device__ __forceinline__ void dw_tile(const DwArgs& a, int j, int w, int s, in
 
 // Both gradients of a piece, which wait for the same g and not for each
 // other, in one launch: the CUs that one's last round leaves idle work on the
-// other.  hn = 0 or wn = 0 leaves one out.
+// other.  All learners' dh, the longer sums, come before all dW.  hn = 0 or
+// wn = 0 leaves one out.
 struct GradsArgs {
   DhArgs h;
   DwArgs w;
+  int k;
   int hn, hs;  // tiles and splits of dh
   int wn, ws;  // of dW
 };
@@ -790,11 +792,18 @@ __global__ __launch_bounds__(TLH::THREADS, 2) void xent_grads(GradsArgs a) {
   extern __shared__ __align__(16) char lds[];
   // dW's tiles start at a multiple of the XCDs, so that tile_of finds them
   // dealt out as it expects
-  const int hall = a.hn * a.hs, from = (hall + NXCD - 1) / NXCD * NXCD, x = blockIdx.x;
-  if (x < hall)
-    dh_tile<TLH>(a.h, blockIdx.y, x % a.hn, x / a.hn, lds);
-  else if (x >= from)
-    dw_tile<TLW>(a.w, blockIdx.y, (x - from) % a.wn, (x - from) / a.wn, a.ws, lds);
+  const int hall = a.hn * a.hs * a.k, from = (hall + NXCD - 1) / NXCD * NXCD;
+  int x = blockIdx.x;
+  if (x < hall) {
+    const int j = x / (a.hn * a.hs);
+    x -= j * a.hn * a.hs;
+    dh_tile<TLH>(a.h, j, x / a.hs, x % a.hs, lds);
+  } else if (x >= from) {
+    x -= from;
+    const int j = x / (a.wn * a.ws);
+    x -= j * a.wn * a.ws;
+    dw_tile<TLW>(a.w, j, x % a.wn, x / a.wn, a.ws, lds);
+  }
 }
 
 // dW from the splits' sums.
@@ -832,7 +841,7 @@ hipError_t launch_grads(GradsArgs a, Plan h, Plan w, int k, hipStream_t s) {
   a.wn = (int)(w.splits ? tiles(a.w.d, a.w.vn, TLW::BP, TLW::BQ) : 0);
   a.hs = h.splits;
   a.ws = w.splits;
-  const dim3 grid((unsigned)(up((int64_t)a.hn * a.hs, NXCD) + (int64_t)a.wn * a.ws), k);
+  const dim3 grid((unsigned)(up((int64_t)a.hn * a.hs * k, NXCD) + (int64_t)a.wn * a.ws * k));
   return launch_with_lds<std::max(TLH::LDS, TLW::LDS), xent_grads<TLH, TLW>>(grid, TLH::THREADS, s,
                                                                              a);
 }
@@ -846,7 +855,7 @@ hipError_t launch_grads(const DhArgs& h, Plan ph, const DwArgs& w, Plan pw, int 
   using WBig = BigTile<T, true, true>;
   using WMid = MidTile<T, true, true>;
   const Plan none{MID, 0};
-  GradsArgs a{h, w, 0, 0, 0, 0};
+  GradsArgs a{h, w, k, 0, 0, 0, 0};
   if (sizeof(T) == 2 && (ph.shape == BIG) != (pw.shape == BIG)) {
     if constexpr (sizeof(T) == 2) {
       if (ph.shape == BIG) {
