@@ -3,7 +3,8 @@
 // read them, taken from the 8 bits.
 //
 // kept_pack and kept_unpack stream: eight columns a thread, four
-// neighbouring threads to a group of 32.
+// neighbouring threads to a group of 32.  16,384 x 4096, bf16 (203 MB each
+// way): 42 and 30 us, 4.8 and 6.7 TB/s, the 8-bit form being in the caches.
 //
 // The weight gradient dW[o][c] = sum_r dy[r][o] x[r][c] runs on the tiles of
 // lm_tile.hpp, with P = x (p = c) and Q = dy (q = o), both in col form; every
@@ -12,10 +13,11 @@
 // columns a thread, one step ahead into registers, converted and written to
 // LDS in the layout that dy's loads have there.  One launch, and for fp32
 // three MFMAs a product instead of six: x is one bf16 number, dy three.
-//   Large layers (tiles of 256): x is unpacked once into the workspace, and
-// the tiles take both operands straight to LDS.  Converting in every one of
-// the out/256 workgroups that read a tile of x costs more (8192 rows, 2048 x
-// 8192, bf16: 240 us against 216 us and 11 us for the unpacking).
+//   Large layers (tiles of 256; 8192 rows, 2048 x 8192, bf16: 1,280 TFLOP/s):
+// x is unpacked once into the workspace, and the tiles take both operands
+// straight to LDS.  Converting in every one of the out/256 workgroups that
+// read a tile of x costs more (240 us there against 216 us and 11 us for the
+// unpacking).
 //   Where the tiles do not fill the CUs, or the last round of them leaves most
 // idle, that round's tiles are shared by workgroups that take some of the rows
 // each, and kept_grad_join adds their sums in order.

@@ -9,8 +9,8 @@
 // fp32 runs on the bf16 matrix cores, sixteen times as fast as the fp32 ones:
 // a float is exactly the sum of three bf16 numbers (its leading 8 bits, the
 // next 8 and the rest), and of the nine products of two such sums the six
-// largest are taken, which leaves out less than fp32's own rounding of the
-// product (2^-23 of it).  The split is made in registers on the way from LDS.
+// largest are taken, which leaves out at most 2^-22 of the product (two of 2^-7
+// times 2^-16) and mostly less than fp32's own rounding of it, 2^-24.  The split is made in registers on the way from LDS.
 // (An infinity splits into an infinity and NaNs: its products are NaN.)
 //
 // A step takes 128 bytes of contraction per row (64 elements of 16 bits or 32
@@ -21,9 +21,10 @@
 // on past its end, which costs no memory traffic.
 //   A 256 x 256 tile of bf16 takes 1.62 us a step, whatever the sum's length
 // (1,300 TFLOP/s over 256 CUs, the library's rate for a large product; the
-// MFMAs alone would need 0.85), and 6.7 us around them.  The matrix cores and
-// LDS are each busy about 60% of it; rings of five steps of half the size,
-// MFMAs pinned before the barrier and raised wave priority were no faster.
+// MFMAs alone would need 0.85), and 6.7 us around them.  The matrix cores are
+// busy 60% of it, and LDS moves 67 of its 128 bytes a cycle; rings of five
+// steps of half the size, MFMAs pinned before the barrier and raised wave
+// priority were no faster, nor, for fp32, splits spread between the MFMAs.
 //
 // Row form in LDS: rows of 128 bytes, the 16-byte chunk c of row r at
 // c ^ (r & 7); a lane's operand of one MFMA is then one conflict-free
@@ -280,9 +281,10 @@ __device__ __forceinline__ void read_frags(const lds_char* lds, int r0, int kk, 
   }
 }
 
-// 32 elements' MFMAs for 16-bit types, while the next operands come from LDS: Q's beside, P's one by one over those that are done with, a few
-// MFMAs between the reads.  VALU: how many vector instructions of
-// what the caller does next to spread over the MFMAs too.
+// 32 elements' MFMAs for 16-bit types, while the next operands come from LDS:
+// Q's beside, P's one by one over those that are done with, a few MFMAs
+// between the reads.  VALU: how many vector instructions of what the caller
+// does next to spread over the MFMAs too.
 template <class T, int RP, bool PCOL, int RQ, bool QCOL, int VALU, int TP, int TQ>
 __device__ __forceinline__ void mma_step(f32x4 (&acc)[TP][TQ], i32x4 (&fp)[TP], i32x4 (&fq)[TQ],
                                           const lds_char* p, const lds_char* q, int wp, int wq,
