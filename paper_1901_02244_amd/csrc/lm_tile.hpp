@@ -10,7 +10,8 @@
 // a float is exactly the sum of three bf16 numbers (its leading 8 bits, the
 // next 8 and the rest), and of the nine products of two such sums the six
 // largest are taken, which leaves out at most 2^-22 of the product (two of 2^-7
-// times 2^-16) and mostly less than fp32's own rounding of it, 2^-24.  The split is made in registers on the way from LDS.
+// times 2^-16) and mostly less than fp32's own rounding of it, 2^-24.  The
+// split is made in registers on the way from LDS.
 // (An infinity splits into an infinity and NaNs: its products are NaN.)
 //
 // A step takes 128 bytes of contraction per row (64 elements of 16 bits or 32
