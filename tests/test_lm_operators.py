@@ -672,6 +672,54 @@ def test_operators_in_a_graph():
             assert torch.equal(want[name], got[name]), (seed, name)
 
 
+def test_operators_on_two_streams_at_once():
+    """Calls that overlap in time, each with workspaces of its own, give what they give alone."""
+    inputs = [step_inputs(BF16, seed) for seed in (5, 6)]
+    want = [learner_step(*a)[0] for a in inputs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(learner_step(*inputs[i])[0])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            for name in want[i]:
+                assert torch.equal(want[i][name], g[name]), (i, name)
+
+
+def test_xent_of_many_rows_in_a_graph():
+    """The labels of a replay are counted anew, chunk by chunk."""
+    n, d, v = 20000, 32, 300
+    gen = torch.Generator("cuda").manual_seed(9)
+    h = torch.randn(1, n, d, generator=gen, device="cuda").to(BF16)
+    w = torch.randn(1, v, d, generator=gen, device="cuda").to(BF16)
+
+    def labels(part):
+        y = torch.randint(0, v, (1, n), generator=gen, device="cuda", dtype=torch.int32)
+        return torch.where(torch.rand(1, n, generator=gen, device="cuda") < part, IGNORE, y).to(torch.int32)
+
+    def step(y):
+        loss, lse = cb.cb_vocab_xent_fwd(h, w, y)
+        return (loss, lse, *cb.cb_vocab_xent_bwd(h, w, y, lse))
+
+    y = labels(0.5)
+    step(y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(y)
+    for part in (0.9, 0.0, 0.3, 1.0):
+        new = labels(part)
+        want = step(new)
+        y.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got)), part
+
+
 def test_workspace_of_the_caller():
     """One workspace for calls in turn, filled with NaN bits before; a short one is refused."""
     import ctypes
