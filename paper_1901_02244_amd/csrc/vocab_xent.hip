@@ -28,7 +28,7 @@
 // them counted, 4096 wide, 128,000 words, both passes: 25.3 ms, 1,220 TFLOP/s of
 // their four products), few by reading W (one row: 172 us for 1.05 GB, 6.1
 // TB/s).  Short sums pay about 10 us around every round of tiles (fp16, two
-// learners of 1023 rows, 1000 wide, 32,001 words: 464 us, 723 TFLOP/s).
+// learners of 1023 rows, 1000 wide, 32,001 words: 427 us, 785 TFLOP/s).
 #include "kept.hpp"
 #include "lm_tile.hpp"
 
@@ -265,16 +265,47 @@ __global__ __launch_bounds__(256) void xent_copy_w(const T* w, int64_t pstride, 
   }
 }
 
+// --- pieces of the vocabulary ----------------------------------------------------
+
+// The backward pass is launched piece by piece, each launch sized for all
+// rows.  Where most rows do not count, a learner takes `m` pieces in a launch
+// (its g then has as many times the words of a fraction of the rows) and is
+// done after fewer; the other launches find nothing to do (8192 rows of 4096,
+// 128,000 words, bf16, of which half count: 10.5 ms against 15.5, a tenth: 3.0
+// against 5.3).
+struct Pieces {
+  int v, piece, index, cap;
+  bool grow;  // else m is 1
+};
+struct Piece {
+  int m, v0, vn;  // vn <= 0: nothing left
+};
+__device__ __forceinline__ Piece piece_of(const Pieces& p, int cnt) {
+  Piece r;
+  r.m = 1;
+  if (p.grow)
+    r.m = max(1, min(p.cap / 256 / max(1, (cnt + 255) / 256), (p.v + p.piece - 1) / p.piece));
+  const int64_t each = (int64_t)p.piece * r.m, v0 = p.index * each;
+  r.v0 = (int)min(v0, (int64_t)p.v);
+  r.vn = (int)min(each, (int64_t)p.v - r.v0);
+  return r;
+}
+// Rows between the splits' sums of dh.
+__device__ __forceinline__ int rows_between(const Pieces& p, const Piece& r, int cnt) {
+  return r.m > 1 ? (cnt + 255) / 256 * 256 : p.cap;
+}
+
 // --- logits --------------------------------------------------------------------
 
 // What xent_logits leaves: the pairs of the loss, g, or a split's sums.
 enum { LOSS, GRAD, SUMS };
 
 struct LogitArgs {
-  const void* w;    // replica 0's first row of the vocabulary range
+  const void* w;
   int64_t ldw, pstride;
   int d;            // width of W's rows that holds values
   int v0, vn;       // the vocabulary range [v0, v0 + vn)
+  Pieces pieces;    // or, for g, the piece's
   const void* hc;   // rows dp apart, a learner's hstride
   int64_t dp, hstride;
   int cap;
@@ -288,7 +319,7 @@ struct LogitArgs {
   // backward
   const float* lse; // [k*n]
   int n;
-  void* g;          // [k][cap][ldg]
+  void* g;          // [k][cap * piece], rows ldg apart
   int ldg;
   // splits of the columns, `span` each
   float* sums;      // [splits][k][cap][lds]
@@ -374,15 +405,24 @@ __device__ __forceinline__ void logits_end(const LogitArgs& a, int j, int cnt, i
 }
 
 template <class TL, int MODE>
-__global__ __launch_bounds__(TL::THREADS, 2) void xent_logits(LogitArgs a) {
+__global__ __launch_bounds__(TL::THREADS, 2) void xent_logits(LogitArgs args) {
   using T = typename TL::T;
   extern __shared__ __align__(16) char lds[];
+  LogitArgs a = args;
   const int j = blockIdx.y, cnt = a.cnt ? a.cnt[j] : a.n;
-  const int np = (a.vn + TL::BP - 1) / TL::BP;
+  if constexpr (MODE == GRAD) {
+    const Piece piece = piece_of(a.pieces, cnt);
+    a.v0 = piece.v0;
+    a.vn = piece.vn;
+    a.w = (const T*)a.w + a.v0 * a.ldw;
+    a.ldg *= piece.m;
+  }
+  // the counted rows' tiles, first of a grid for all rows
+  const int np = (a.vn + TL::BP - 1) / TL::BP, nq = (cnt + TL::BQ - 1) / TL::BQ;
+  if (a.vn <= 0 || (int)blockIdx.x >= np * nq) return;
   int tp, tq;
-  tile_of<8>(blockIdx.x, np, gridDim.x / np, tp, tq);
+  tile_of<8>(blockIdx.x, np, nq, tp, tq);
   const int p0 = tp * TL::BP, q0 = tq * TL::BQ;
-  if (q0 >= cnt) return;
   const Operand<T> W{(const T*)a.w + j * a.pstride, a.ldw, a.vn, a.d};
   const Operand<T> H{(const T*)a.hc + j * a.hstride, a.dp, cnt, a.d};
   typename TL::Acc acc;
@@ -430,7 +470,7 @@ __global__ __launch_bounds__(TL::THREADS, 2) void xent_logits(LogitArgs a) {
     // words by sixteen rows a wave
     constexpr int CPR = TL::BP * (int)sizeof(T) / 16, EACH = TL::BQ * CPR / TL::THREADS;
     static_assert(EACH * TL::THREADS == TL::BQ * CPR && TL::BQ * CPR * 16 <= TL::LDS, "");
-    T* g = (T*)a.g + ((int64_t)j * a.cap + q0) * a.ldg + p0;
+    T* g = (T*)a.g + (int64_t)j * a.cap * a.pieces.piece + (int64_t)q0 * a.ldg + p0;
 #pragma unroll 4
     for (int i = 0; i < EACH; ++i) {
       const int id = i * TL::THREADS + threadIdx.x, x = id / CPR, c = id % CPR;
@@ -680,44 +720,52 @@ __global__ __launch_bounds__(256) void xent_mean_join(const double2* means, int 
 // --- gradients -------------------------------------------------------------------
 
 struct DhArgs {
-  const void* w;    // the piece's first row
+  const void* w;
   int64_t ldw, pstride;
-  int dw, vn;       // columns of W that can be read
+  int dw;           // columns of W that can be read
+  Pieces pieces;
   const void* g;
-  int ldg, cap;
+  int ldg;
   const int *cnt, *row;
-  float* sums;      // [splits][k][cap][dp]
-  int dp, span;     // a split takes `span` words
-  int64_t split_stride;
-  int add;          // to what the pieces before left in sums
+  float* sums;      // [k][splits * cap][dp]
+  int dp, splits;
   void* dh;         // the results themselves, [k*n][d], or nullptr
   int n, d, vec;
   float scale;
 };
 
-// One tile, the w-th of the learner's, of split s of dh: P = W in col form
-// (p = column), Q = g in row form (q = row).
+// The x-th workgroup of learner j: P = W in col form (p = column), Q = g in
+// row form (q = row).  A learner that takes m pieces at once has m times the
+// splits, of an m-th of the rows; the last piece of one that needs none
+// writes dh itself.
 template <class TL>
-__device__ __forceinline__ void dh_tile(const DhArgs& a, int j, int w, int s, char* lds) {
+__device__ __forceinline__ void dh_tile(const DhArgs& a, int j, int x, char* lds) {
   using T = typename TL::T;
-  const int cnt = a.cnt[j];
+  const int cnt = a.cnt[j], cap = a.pieces.cap;
+  const Piece piece = piece_of(a.pieces, cnt);
+  const int np = (a.d + TL::BP - 1) / TL::BP, nq = (cnt + TL::BQ - 1) / TL::BQ;
+  const int splits = a.splits * piece.m, ldg = a.ldg * piece.m;
+  if (piece.vn <= 0 || x >= np * nq * splits) return;
+  const int s = x % splits, span = ((piece.vn + splits - 1) / splits + 63) / 64 * 64;
   int tp, tq;
-  tile_of<8>(w, (a.d + TL::BP - 1) / TL::BP, (a.n + TL::BQ - 1) / TL::BQ, tp, tq);
+  tile_of<8>(x / splits, np, nq, tp, tq);
   const int p0 = tp * TL::BP, q0 = tq * TL::BQ;
-  if (q0 >= cnt) return;
-  const Operand<T> W{(const T*)a.w + j * a.pstride, a.ldw, a.dw, a.vn};
-  const Operand<T> G{(const T*)a.g + (int64_t)j * a.cap * a.ldg, a.ldg, cnt, a.vn};
+  const Operand<T> W{(const T*)a.w + j * a.pstride + piece.v0 * a.ldw, a.ldw, a.dw, piece.vn};
+  const Operand<T> G{(const T*)a.g + (int64_t)j * cap * a.pieces.piece, ldg, cnt, piece.vn};
   typename TL::Acc acc;
-  TL::product(W, G, p0, q0, min(s * a.span, a.vn), min((s + 1) * a.span, a.vn), lds, acc);
-  float* sums = a.sums + s * a.split_stride + (int64_t)j * a.cap * a.dp;
+  TL::product(W, G, p0, q0, min(s * span, piece.vn), min((s + 1) * span, piece.vn), lds, acc);
+  float* sums = a.sums + ((int64_t)j * a.splits * cap +
+                          (int64_t)s * rows_between(a.pieces, piece, cnt)) * a.dp;
   const float f = a.scale / max(cnt, 1);
+  const bool add = a.pieces.index > 0;
+  T* dh = splits == 1 && piece.v0 + piece.vn == a.pieces.v ? (T*)a.dh : nullptr;
   TL::for_each_quad(acc, [&](int p, int q, f32x4 v) {
     if (q0 + q >= cnt || p0 + p >= a.d) return;
     f32x4* at = (f32x4*)(sums + (int64_t)(q0 + q) * a.dp + p0 + p);
-    if (a.add) v = *at + v;
-    if (a.dh)
-      store4<T>((T*)a.dh + ((int64_t)j * a.n + a.row[(int64_t)j * a.cap + q0 + q]) * a.d + p0 + p,
-                v, f, a.d - p0 - p, a.vec);
+    if (add) v = *at + v;
+    if (dh)
+      store4<T>(dh + ((int64_t)j * a.n + a.row[(int64_t)j * cap + q0 + q]) * a.d + p0 + p, v, f,
+                a.d - p0 - p, a.vec);
     else
       *at = v;
   });
@@ -726,60 +774,71 @@ __device__ __forceinline__ void dh_tile(const DhArgs& a, int j, int w, int s, ch
 // dh from the splits' sums, four neighbouring columns a thread; zero where
 // the label is ignored.
 template <class T>
-__global__ __launch_bounds__(256) void xent_dh(const float* sums, int splits, int64_t split_stride,
-                                               const int* pos, const int* cnt, int n, int d,
-                                               int dp, int cap, float scale, T* dh) {
-  const int j = blockIdx.y, quads = (d + 3) / 4;
-  const float f = scale / max(cnt[j], 1);
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < (int64_t)n * quads;
+__global__ __launch_bounds__(256) void xent_dh(DhArgs a, const int* pos) {
+  const int j = blockIdx.y, quads = (a.d + 3) / 4, cnt = a.cnt[j];
+  const Piece piece = piece_of(a.pieces, cnt);
+  const int splits = a.splits * piece.m;
+  if (splits == 1) return;  // written already
+  const float f = a.scale / max(cnt, 1);
+  const float* sums = a.sums + (int64_t)j * a.splits * a.pieces.cap * a.dp;
+  const int64_t stride = (int64_t)rows_between(a.pieces, piece, cnt) * a.dp;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < (int64_t)a.n * quads;
        i += gridDim.x * 256ll) {
     const int64_t r = i / quads;
-    const int x = (int)(i - r * quads) * 4, p = pos[(int64_t)j * n + r];
+    const int x = (int)(i - r * quads) * 4, p = pos[(int64_t)j * a.n + r];
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (p >= 0) v = sum4(sums + ((int64_t)j * cap + p) * dp + x, splits, split_stride);
-    store4<T>(dh + ((int64_t)j * n + r) * d + x, v, f, d - x, false);
+    if (p >= 0) v = sum4(sums + (int64_t)p * a.dp + x, splits, stride);
+    store4<T>((T*)a.dh + ((int64_t)j * a.n + r) * a.d + x, v, f, a.d - x, false);
   }
 }
 
 struct DwArgs {
   const void* hc;
-  int dp, cap, d, vn;
+  int dp, d, vn;    // vn: of a piece with m = 1
+  Pieces pieces;
   const void* g;
   int ldg;
   const int* cnt;
   float scale;
-  void* dw;         // the piece's first row
+  void* dw;
   int64_t dstride;
   int vec;          // rows start on 4 elements
   float* sums;      // [splits][k][vn][dp], or nullptr: write dw
   int64_t split_stride;
 };
 
-// One tile of split s of the piece's rows of dW: P = h in col form (p =
-// column), Q = g in col form (q = word).
+// Split s of tile x of the piece's rows of dW, and, of a learner that takes m
+// pieces at once, of every `all`-th after it: P = h in col form (p = column),
+// Q = g in col form (q = word).
 template <class TL>
-__device__ __forceinline__ void dw_tile(const DwArgs& a, int j, int w, int s, int splits,
-                                        char* lds) {
+__device__ __forceinline__ void dw_tiles(const DwArgs& a, int j, int x, int all, int s, int splits,
+                                         char* lds) {
   using T = typename TL::T;
-  const int cnt = a.cnt[j];
-  int tp, tq;
-  tile_of<8>(w, (a.d + TL::BP - 1) / TL::BP, (a.vn + TL::BQ - 1) / TL::BQ, tp, tq);
-  const int p0 = tp * TL::BP, q0 = tq * TL::BQ;
-  const Operand<T> H{(const T*)a.hc + (int64_t)j * a.cap * a.dp, a.dp, a.dp, cnt};
-  const Operand<T> G{(const T*)a.g + (int64_t)j * a.cap * a.ldg, a.ldg, a.ldg, cnt};
-  typename TL::Acc acc;
+  const int cnt = a.cnt[j], cap = a.pieces.cap;
+  const Piece piece = piece_of(a.pieces, cnt);
+  if (piece.vn <= 0) return;
+  const int np = (a.d + TL::BP - 1) / TL::BP, nq = (piece.vn + TL::BQ - 1) / TL::BQ;
+  const int ldg = a.ldg * piece.m;
+  const Operand<T> H{(const T*)a.hc + (int64_t)j * cap * a.dp, a.dp, a.dp, cnt};
+  const Operand<T> G{(const T*)a.g + (int64_t)j * cap * a.pieces.piece, ldg, ldg, cnt};
   const int span = (((cnt + splits - 1) / splits) + TL::BK - 1) / TL::BK * TL::BK;
-  TL::product(H, G, p0, q0, min(s * span, cnt), min((s + 1) * span, cnt), lds, acc);
   const float f = a.scale / max(cnt, 1);
-  T* out = (T*)a.dw + j * a.dstride;
+  T* out = (T*)a.dw + j * a.dstride + (int64_t)piece.v0 * a.d;
   float* sums = a.sums ? a.sums + s * a.split_stride + (int64_t)j * a.vn * a.dp : nullptr;
-  TL::for_each_quad(acc, [&](int p, int q, f32x4 v) {
-    if (q0 + q >= a.vn || p0 + p >= a.d) return;
-    if (sums)
-      *(f32x4*)(sums + (int64_t)(q0 + q) * a.dp + p0 + p) = v;
-    else
-      store4<T>(out + (int64_t)(q0 + q) * a.d + p0 + p, v, f, a.d - p0 - p, a.vec);
-  });
+  for (; x < np * nq; x += all) {
+    int tp, tq;
+    tile_of<8>(x, np, nq, tp, tq);
+    const int p0 = tp * TL::BP, q0 = tq * TL::BQ;
+    typename TL::Acc acc;
+    TL::product(H, G, p0, q0, min(s * span, cnt), min((s + 1) * span, cnt), lds, acc);
+    TL::for_each_quad(acc, [&](int p, int q, f32x4 v) {
+      if (q0 + q >= piece.vn || p0 + p >= a.d) return;
+      if (sums)
+        *(f32x4*)(sums + (int64_t)(q0 + q) * a.dp + p0 + p) = v;
+      else
+        store4<T>(out + (int64_t)(q0 + q) * a.d + p0 + p, v, f, a.d - p0 - p, a.vec);
+    });
+  }
 }
 
 // Both gradients of a piece, which wait for the same g and not for each
@@ -804,12 +863,12 @@ __global__ __launch_bounds__(TLH::THREADS, 2) void xent_grads(GradsArgs a) {
   if (x < hall) {
     const int j = x / (a.hn * a.hs);
     x -= j * a.hn * a.hs;
-    dh_tile<TLH>(a.h, j, x / a.hs, x % a.hs, lds);
+    dh_tile<TLH>(a.h, j, x, lds);
   } else if (x >= from) {
     x -= from;
     const int j = x / (a.wn * a.ws);
     x -= j * a.wn * a.ws;
-    dw_tile<TLW>(a.w, j, x % a.wn, x / a.wn, a.ws, lds);
+    dw_tiles<TLW>(a.w, j, x % a.wn, a.wn, x / a.wn, a.ws, lds);
   }
 }
 
@@ -823,7 +882,7 @@ __global__ __launch_bounds__(256) void xent_dw_join(DwArgs a, int splits) {
     const int64_t q = i / quads;
     const int p = (int)(i - q * quads) * 4;
     const f32x4 v = sum4(a.sums + ((int64_t)j * a.vn + q) * a.dp + p, splits, a.split_stride);
-    store4<T>((T*)a.dw + j * a.dstride + q * a.d + p, v, f, a.d - p, a.vec);
+    store4<T>((T*)a.dw + j * a.dstride + ((int64_t)a.pieces.index * a.pieces.piece + q) * a.d + p, v, f, a.d - p, a.vec);
   }
 }
 
@@ -1005,11 +1064,16 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
   if (hipError_t e = prepare<T>(a, l, true, direct, g, s)) return e;
   g.g = ws + l.g;
   g.ldg = l.piece;
+  // several pieces, and room for a learner with half of the rows or fewer to
+  // take more than one (dW's splits have sums for one)
+  const bool grow = a.v > l.piece && l.cap >= 512 && l.dw.splits == 1;
+  g.pieces = Pieces{a.v, l.piece, 0, l.cap, grow};
   const float scale = a.grad_scale / g_scale<T>();
   auto quads = [&](const void* p, int64_t stride) {
     return a.d % 4 == 0 && (uintptr_t)p % (4 * sizeof(T)) == 0 && stride % 4 == 0;
   };
   DhArgs dh{};
+  dh.w = g.w;
   dh.ldw = g.ldw;
   dh.pstride = g.pstride;
   dh.dw = g.d;
@@ -1017,18 +1081,18 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
   dh.n = a.n;
   dh.g = g.g;
   dh.ldg = l.piece;
-  dh.cap = l.cap;
   dh.cnt = g.cnt;
   dh.row = g.row;
   dh.sums = (float*)(ws + l.dhsum);
   dh.dp = l.dp;
-  dh.split_stride = (int64_t)a.k * l.cap * l.dp;
+  dh.splits = l.dh.splits;
+  dh.dh = a.dh;
   dh.vec = quads(a.dh, 0);
   dh.scale = scale;
   DwArgs dw{};
   dw.hc = g.hc;
   dw.dp = l.dp;
-  dw.cap = l.cap;
+  dw.dw = a.dw;
   dw.d = a.d;
   dw.g = g.g;
   dw.ldg = l.piece;
@@ -1037,11 +1101,8 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
   dw.dstride = a.dstride;
   dw.vec = quads(a.dw, a.dstride);
   dw.sums = l.dw.splits > 1 ? (float*)(ws + l.dwsum) : nullptr;
-  const T* w = (const T*)g.w;
   for (int v0 = 0; v0 < a.v; v0 += l.piece) {
     const int vn = std::min(l.piece, a.v - v0);
-    g.w = w + v0 * g.ldw;
-    g.v0 = v0;
     g.vn = vn;
     if (l.logits.splits > 1) {
       if (hipError_t e = launch_logits<T, SUMS>(g, l.logits, a.k, a.n, s)) return e;
@@ -1069,14 +1130,9 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
       p.splits = 1;
       if (hipError_t e = launch_logits<T, GRAD>(g, p, a.k, a.n, s)) return e;
     }
-    dh.w = g.w;
-    dh.vn = vn;
-    dh.span = (int)up((vn + l.dh.splits - 1) / l.dh.splits, 64);
-    dh.add = v0 > 0;
-    dh.dh = v0 + vn == a.v ? direct : nullptr;
+    dh.pieces = dw.pieces = g.pieces;
     dw.vn = vn;
     dw.split_stride = (int64_t)a.k * vn * l.dp;
-    dw.dw = (T*)a.dw + (int64_t)v0 * a.d;
     const Plan pw = l.dw.splits > 1 ? l.dw : plan(a.type, a.k, a.d, vn, 0, false, false);
     if (hipError_t e = launch_grads<T>(dh, l.dh, dw, pw, a.k, s)) return e;
     if (dw.sums) {
@@ -1085,12 +1141,12 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
               s, dw, l.dw.splits);
       if (hipError_t e2 = hipGetLastError()) return e2;
     }
+    ++g.pieces.index;
   }
-  if (direct) return hipSuccess;
+  if (l.dh.splits == 1 && !grow) return hipSuccess;
   const int64_t blocks = ((int64_t)a.n * ((a.d + 3) / 4) + 255) / 256;
-  klaunch(xent_dh<T>, dim3((unsigned)std::min<int64_t>(blocks, 4096), a.k), dim3(256), 0, s,
-          (const float*)dh.sums, l.dh.splits, dh.split_stride, (const int*)(ws + l.pos), g.cnt,
-          a.n, a.d, l.dp, l.cap, scale, (T*)a.dh);
+  klaunch(xent_dh<T>, dim3((unsigned)std::min<int64_t>(blocks, 4096), a.k), dim3(256), 0, s, dh,
+          (const int*)(ws + l.pos));
   return hipGetLastError();
 }
 

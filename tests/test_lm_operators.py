@@ -184,6 +184,28 @@ def test_xent_pieces():
     xent_check(h, w, y)
 
 
+@pytest.mark.parametrize("t", [F32, BF16], ids=str)
+@pytest.mark.parametrize("d", [200, 1000])
+def test_xent_pieces_of_few_counted_rows(d, t):
+    """Learners that need one, two and all of the launches of a pass in pieces, and one that counts nothing."""
+    k, n, v = 5, 1100, 30000
+    gen = torch.Generator("cuda").manual_seed(d)
+    h = torch.randn(k, n, d, generator=gen, device="cuda").to(t)
+    w = (torch.randn(k, v, d, generator=gen, device="cuda") * d ** -0.5).to(t)
+    y = torch.randint(0, v, (k, n), generator=gen, device="cuda", dtype=torch.int32)
+    for j, part in enumerate((0.9, 0.55, 0.0, 1.0, 0.7)):
+        y[j][torch.rand(n, generator=gen, device="cuda") < part] = IGNORE
+    h[0][y[0] == IGNORE] = torch.nan
+    loss, lse = cb.cb_vocab_xent_fwd(h, w, y)
+    dh, dw = cb.cb_vocab_xent_bwd(h, w, y, lse, grad_scale=3.0)
+    h[0][y[0] == IGNORE] = 0
+    for j in range(k):
+        want = ref.xent(h[j], w[j], y[j], IGNORE, 3.0)
+        for name, got in (("loss", loss), ("lse", lse), ("dh", dh), ("dw", dw)):
+            x, bound = want[name]
+            close(f"{name}[{j}]", got[j], (torch.as_tensor(x).cpu(), torch.as_tensor(bound).cpu()))
+
+
 @pytest.mark.parametrize("t", TYPES, ids=str)
 def test_xent_strides(t):
     """h a slice of wider rows, W and dW slices of flat parameter vectors, at places with and
