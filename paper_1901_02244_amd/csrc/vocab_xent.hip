@@ -95,7 +95,8 @@ struct Layout {
   int cap;       // rows of a learner, up to a multiple of 64
   int dp;        // columns of the gathered rows, up to a multiple of 128 bytes
   int piece;     // vocabulary rows of one piece of the backward pass
-  int parts;     // tiles of the vocabulary, each with a (max, sum) of a row
+  int words;     // of a tile of the forward's logits
+  int parts;     // such tiles, each with a (max, sum) of a row
   Plan logits, dh, dw;
   bool copy_w;
   size_t cnt, chunks, pos, row, lab, hc, wc, part, plog, rloss, means, g, lsum, dhsum, dwsum,
@@ -122,7 +123,16 @@ Layout layout(const XentArgs& a, bool backward) {
   const int64_t fit = (int64_t(128) << 20) / (rows * sz) / 256 * 256;
   l.piece = (int)std::min<int64_t>(up(v, 256), std::max<int64_t>(4096, fit));
   l.logits = plan_logits(a.type, k, n, d, v);
-  l.parts = (int)(up(v, bp_of(l.logits.shape)) / bp_of(l.logits.shape));
+  // THIN tiles behind a full round take the time of their sum and not of their
+  // words: two rounds and more share the words evenly (bf16, one row of 3968,
+  // 132,096 words: 184 us against 239 with 4 tiles behind 512; 4096 wide,
+  // 262,144 words, two full rounds either way: 353)
+  l.words = bp_of(l.logits.shape);
+  const int64_t rounds = (tiles_of(THIN, k, v, n) + 511) / 512;
+  if (l.logits.shape == THIN && rounds > 1)
+    l.words = (int)std::min<int64_t>(
+        l.words, up((v * (int64_t)k + rounds * 512 - 1) / (rounds * 512), 16));
+  l.parts = (int)(up(v, l.words) / l.words);
   l.dh = plan(a.type, k, d, n, std::min(l.piece, v), true, true);
   l.dw = plan(a.type, k, d, std::min(l.piece, v), n, false, true);
   // logits in shares only where they are few, which are one piece
@@ -315,7 +325,7 @@ struct LogitArgs {
   // forward
   float2* part;     // [k][parts][cap]
   float* plog;      // [k][cap]
-  int parts;
+  int parts, words;
   // backward
   const float* lse; // [k*n]
   int n;
@@ -418,11 +428,13 @@ __global__ __launch_bounds__(TL::THREADS, 2) void xent_logits(LogitArgs args) {
     a.ldg *= piece.m;
   }
   // the counted rows' tiles, first of a grid for all rows
-  const int np = (a.vn + TL::BP - 1) / TL::BP, nq = (cnt + TL::BQ - 1) / TL::BQ;
+  const int words = MODE == LOSS ? a.words : TL::BP;
+  const int np = (a.vn + words - 1) / words, nq = (cnt + TL::BQ - 1) / TL::BQ;
   if (a.vn <= 0 || (int)blockIdx.x >= np * nq) return;
   int tp, tq;
   tile_of<8>(blockIdx.x, np, nq, tp, tq);
-  const int p0 = tp * TL::BP, q0 = tq * TL::BQ;
+  const int p0 = tp * words, q0 = tq * TL::BQ;
+  if constexpr (MODE == LOSS) a.vn = min(a.vn, p0 + words);
   const Operand<T> W{(const T*)a.w + j * a.pstride, a.ldw, a.vn, a.d};
   const Operand<T> H{(const T*)a.hc + j * a.hstride, a.dp, cnt, a.d};
   typename TL::Acc acc;
@@ -898,7 +910,8 @@ hipError_t launch_logits(const LogitArgs& a, Plan p, int k, int n, hipStream_t s
   if constexpr (sizeof(T) == 2 && MODE != SUMS)
     if (p.shape == BIG) return launch_tile<Big, xent_logits<Big, MODE>>(a.vn, n, k, p.splits, s, a);
   if (p.shape == MID) return launch_tile<Mid, xent_logits<Mid, MODE>>(a.vn, n, k, p.splits, s, a);
-  return launch_tile<Thin, xent_logits<Thin, MODE>>(a.vn, n, k, p.splits, s, a);
+  const int64_t v = MODE == LOSS ? (int64_t)a.parts * Thin::BP : a.vn;
+  return launch_tile<Thin, xent_logits<Thin, MODE>>(v, n, k, p.splits, s, a);
 }
 
 template <class TLH, class TLW>
@@ -1016,6 +1029,7 @@ hipError_t forward(const XentArgs& a, hipStream_t s) {
   g.part = (float2*)(ws + l.part);
   g.plog = (float*)(ws + l.plog);
   g.parts = l.parts;
+  g.words = l.words;
   // up to 64 rows one workgroup takes all, and their mean; a wave a row fills
   // the card up to some thousands; the pairs of more rows are read best side
   // by side

@@ -207,6 +207,13 @@ def test_xent_pieces_of_few_counted_rows(d, t):
 
 
 @pytest.mark.parametrize("t", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(1, 3, 64, 140001), (2, 5, 40, 70001), (1, 1, 16, 131073), (3, 32, 24, 90000)], ids=str)
+def test_xent_few_rows_many_words(size, t):
+    """More tiles of few rows than run together."""
+    xent_check(*xent_inputs(*size, t))
+
+
+@pytest.mark.parametrize("t", TYPES, ids=str)
 def test_xent_strides(t):
     """h a slice of wider rows, W and dW slices of flat parameter vectors, at places with and
     without 16-byte alignment; what lies between stays as it was."""
