@@ -130,8 +130,7 @@ Layout layout(const XentArgs& a, bool backward) {
   l.words = bp_of(l.logits.shape);
   const int64_t rounds = (tiles_of(THIN, k, v, n) + 511) / 512;
   if (l.logits.shape == THIN && rounds > 1)
-    l.words = (int)std::min<int64_t>(
-        l.words, up((v * (int64_t)k + rounds * 512 - 1) / (rounds * 512), 16));
+    l.words = (int)std::min<int64_t>(l.words, up(up(v, rounds * 512 / k) / (rounds * 512 / k), 16));
   l.parts = (int)(up(v, l.words) / l.words);
   l.dh = plan(a.type, k, d, n, std::min(l.piece, v), true, true);
   l.dw = plan(a.type, k, d, std::min(l.piece, v), n, false, true);
