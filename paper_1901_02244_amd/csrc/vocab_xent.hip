@@ -893,7 +893,8 @@ __global__ __launch_bounds__(256) void xent_dw_join(DwArgs a, int splits) {
     const int64_t q = i / quads;
     const int p = (int)(i - q * quads) * 4;
     const f32x4 v = sum4(a.sums + ((int64_t)j * a.vn + q) * a.dp + p, splits, a.split_stride);
-    store4<T>((T*)a.dw + j * a.dstride + ((int64_t)a.pieces.index * a.pieces.piece + q) * a.d + p, v, f, a.d - p, a.vec);
+    const int64_t word = (int64_t)a.pieces.index * a.pieces.piece + q;
+    store4<T>((T*)a.dw + j * a.dstride + word * a.d + p, v, f, a.d - p, a.vec);
   }
 }
 
@@ -959,7 +960,8 @@ hipError_t prepare(const XentArgs& a, const Layout& l, bool gather, void* dh, Lo
                    hipStream_t s) {
   char* ws = (char*)a.ws;
   RowsArgs r{a.h, a.ldh, a.labels, a.ignore, a.n, a.d, l.dp, l.cap,
-             a.n > MANY ? (int*)(ws + l.chunks) : nullptr, (int*)(ws + l.cnt), (int*)(ws + l.pos), (int*)(ws + l.row), (int*)(ws + l.lab),
+             a.n > MANY ? (int*)(ws + l.chunks) : nullptr,
+             (int*)(ws + l.cnt), (int*)(ws + l.pos), (int*)(ws + l.row), (int*)(ws + l.lab),
              ws + l.hc, dh};
   if (gather) {
     // a row a wave, unless that makes the counting dear
