@@ -150,7 +150,7 @@ struct KeptTile {
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       const int id = u * THREADS + threadIdx.x, row = id / UPR, c = id % UPR * 2;
-      const float s = kept_scale(b.e[u]), low = -128.f * s;
+      const float s = kept_scale(b.e[u]);
       const int swz = col_swizzle<BP * 2 / 16>(row);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -158,12 +158,13 @@ struct KeptTile {
         i32x4 o;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          // bytes of q + 128, times 2^e, less 128 * 2^e: exact, and conversions
-          // of unsigned bytes are single instructions
-          const uint32_t w = (uint32_t)b.q[u][2 * h + i / 2] ^ 0x80808080u;
+          // the product alone, which is exact at every 2^e: 128 * 2^e, that an
+          // offset of the bytes would bring in, is past fp32's largest value
+          // for the two largest e
+          const uint32_t w = (uint32_t)b.q[u][2 * h + i / 2];
           const int sh = i % 2 * 16;
-          const float x0 = __builtin_fmaf((float)(w >> sh & 0xffu), s, low);
-          const float x1 = __builtin_fmaf((float)(w >> (sh + 8) & 0xffu), s, low);
+          const float x0 = (float)(int8_t)(w >> sh) * s;
+          const float x1 = (float)(int8_t)(w >> (sh + 8)) * s;
           if constexpr (__is_same(Half, __bf16)) {
             o[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x1),
                                          __builtin_bit_cast(uint32_t, x0), 0x07060302);

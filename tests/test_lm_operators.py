@@ -616,6 +616,26 @@ def test_ckpt_wgrad_of_nan(t):
     assert torch.equal(dw[0, :, :32], clean[0, :, :32]) and torch.equal(dw[0, :, 64:], clean[0, :, 64:])
 
 
+@pytest.mark.parametrize("t", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(2, 40, 96, 40), (1, 130, 4104, 4100)], ids=str)
+def test_ckpt_wgrad_of_the_largest_values(size, t):
+    """Groups up to the type's largest value, zeros and small values among them, at both tile sizes: dw is the
+    product of what unpacking gives."""
+    k, n, d, out = size
+    gen = torch.Generator().manual_seed(12)
+    x, dy = rand(gen, *size[:3], t=t), rand(gen, k, n, out, std=2.0 ** -10, t=t)
+    most = torch.finfo(t).max
+    x[:, 0::5, 0::32], x[:, 1::5, 3::32], x[:, 2::5, 7::32], x[:, 3::5, 9::32] = most, -most, 0.6 * most, -0.3 * most
+    x[:, :, 11::32] = 0
+    dy[:, :, 5] = 0
+    kept = cb.cb_ckpt_pack(x.cuda())
+    values = cb.cb_ckpt_unpack(kept).cpu()
+    assert torch.isfinite(values).all()
+    dw = cb.cb_ckpt_wgrad(kept, dy.cuda())
+    for j in range(k):
+        close(f"dw[{j}]", dw[j], ref.wgrad(values[j], dy[j])["dw"])
+
+
 # --- together, streams, graphs ------------------------------------------------------
 
 def learner_step(x, o, wo, gate, post, pre, w, y):
