@@ -284,16 +284,14 @@ __global__ __launch_bounds__(256) void xent_copy_w(const T* w, int64_t pstride, 
 // against 5.3).
 struct Pieces {
   int v, piece, index, cap;
-  bool grow;  // else m is 1
+  int most;  // the largest m
 };
 struct Piece {
   int m, v0, vn;  // vn <= 0: nothing left
 };
 __device__ __forceinline__ Piece piece_of(const Pieces& p, int cnt) {
   Piece r;
-  r.m = 1;
-  if (p.grow)
-    r.m = max(1, min(p.cap / 256 / max(1, (cnt + 255) / 256), (p.v + p.piece - 1) / p.piece));
+  r.m = max(1, min(p.cap / 256 / max(1, (cnt + 255) / 256), p.most));
   const int64_t each = (int64_t)p.piece * r.m, v0 = p.index * each;
   r.v0 = (int)min(v0, (int64_t)p.v);
   r.vn = (int)min(each, (int64_t)p.v - r.v0);
@@ -1082,7 +1080,11 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
   // several pieces, and room for a learner with half of the rows or fewer to
   // take more than one (dW's splits have sums for one)
   const bool grow = a.v > l.piece && l.cap >= 512 && l.dw.splits == 1;
-  g.pieces = Pieces{a.v, l.piece, 0, l.cap, grow};
+  // and g's rows lie no further apart than lets a tile of 256 stay below 2 GiB:
+  // what a tile's 31-bit offsets do not reach would read as zero
+  const int64_t fits = INT_MAX / ((int64_t)l.piece * sizeof(T) * 256);
+  const int64_t most = grow ? std::min(up(a.v, l.piece) / l.piece, fits) : 1;
+  g.pieces = Pieces{a.v, l.piece, 0, l.cap, (int)most};
   const float scale = a.grad_scale / g_scale<T>();
   auto quads = [&](const void* p, int64_t stride) {
     return a.d % 4 == 0 && (uintptr_t)p % (4 * sizeof(T)) == 0 && stride % 4 == 0;

@@ -141,6 +141,41 @@ def test_xent_past_four_gib(t):
     assert ((got - exp).abs() <= 3 * u * f * (g.abs() @ tail.double().abs()) + 1e-5).all()
 
 
+@pytest.mark.parametrize("t", [F16, BF16], ids=str)
+def test_xent_few_counted_rows_of_many_words(t):
+    """250 of 300,000 rows count, of 5,000,000 words: all the pieces that a launch could take together would make
+    g's rows 9.6 MB apart, and 250 of those pass 2 GiB.  All words but the last 300 are zero."""
+    n, d, v, m, c = 300000, 2304, 5000000, 300, 250
+    gen = torch.Generator().manual_seed(10)
+    tail = rand(gen, m, d, std=0.05, t=t)
+    w = torch.zeros(1, v, d, dtype=t, device="cuda")
+    w[0, v - m:] = tail.cuda()
+    h = torch.zeros(1, n, d, dtype=t, device="cuda")
+    y = torch.full((1, n), IGNORE, dtype=torch.int32, device="cuda")
+    at = torch.arange(c) * 1199 + 7
+    rows, hit = rand(gen, c, d, t=t), torch.randint(0, m, (c,), generator=gen)
+    h[0, at.cuda()] = rows.cuda()
+    y[0, at.cuda()] = (v - m + hit).int().cuda()
+    loss, lse = cb.cb_vocab_xent_fwd(h, w, y)
+    dh, dw = cb.cb_vocab_xent_bwd(h, w, y, lse, grad_scale=float(c))
+    H, W = rows.double(), tail.double()
+    logits = H @ W.T
+    want = torch.log((v - m) + logits.exp().sum(1))
+    # fp32 sums of 5,000,000 terms, tile by tile: 24 roundings deep at the most, as many more for the logits
+    assert ((lse[0, at.cuda()].cpu().double() - want).abs() < 1e-5).all()
+    assert abs(loss[0].item() - (want - logits[torch.arange(c), hit]).mean().item()) < 1e-5
+    g = (logits - want[:, None]).exp()
+    g[torch.arange(c), hit] -= 1
+    u = ref.u(t)
+    # g is rounded to its type and the result once more; 1e-5 is lse's own error, 1e-7 fp16's subnormals
+    got, exp = dh[0, at.cuda()].cpu().double(), g @ W
+    assert ((got - exp).abs() <= (3 * u + 1e-5) * (g.abs() @ W.abs()) + 1e-7).all()
+    got, exp = dw[0, v - m:].cpu().double(), g.T @ H
+    assert ((got - exp).abs() <= (3 * u + 1e-5) * (g.abs().T @ H.abs()) + 1e-7).all()
+    dh[0, at.cuda()] = 0
+    assert (dh == 0).all()
+
+
 @pytest.mark.parametrize("t", TYPES, ids=str)
 def test_xent_label_out_of_range(t):
     """As in cb_step: the learner's loss is NaN, the gradient has no one-hot term."""
