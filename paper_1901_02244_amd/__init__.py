@@ -373,9 +373,10 @@ class Context:
 # Tensors of k learners: activations [k, n, width], parameters and gradients with
 # the learner as their first dimension, which may be strided (a slice of a flat
 # [k, P] vector).  Outputs are allocated on the inputs' device; the work goes to
-# `stream`, or to torch's current stream of that device.  A workspace is a uint8
-# tensor that the caller keeps; without one each call takes its own from torch's
-# allocator.
+# `stream`, or to torch's current stream of that device.  `stream` waits for nothing by
+# itself: the caller has it wait for the inputs, and waits for it before using the
+# outputs.  A workspace is a uint8 tensor that the caller keeps; without one each call
+# takes its own from torch's allocator.
 
 def _refuse(who, why):
     raise CBError(CB_EINVAL, f"{who}: {why}")
@@ -423,9 +424,11 @@ def _outer(t):
 
 
 def _begin(t, stream):
-    """Makes the device of t current.  Returns the handle of the call's stream, that
-    stream where it is not torch's current one (the allocator has to know that new
-    tensors are used there) or None, and the device to return to or -1."""
+    """Makes the device of t current, and `stream` if one is given, so that new tensors
+    are that stream's memory: a block of another stream's may have been freed while
+    work queued there still reads it.  Returns the handle of the call's stream, what
+    was torch's current stream (where results are used next, which the allocator has
+    to know) if it was another one or None, and the device to return to or -1."""
     cuda, index = _torch.cuda, t.get_device()
     back = cuda.current_device()
     if back != index:
@@ -435,10 +438,14 @@ def _begin(t, stream):
     here = _current_stream(index)
     if stream is None or stream.cuda_stream == here:
         return here, None, back
-    return stream.cuda_stream, stream, back
+    before = cuda.current_stream(index)
+    cuda.set_stream(stream)
+    return stream.cuda_stream, before, back
 
 
-def _end(back):
+def _end(before, back):
+    if before is not None:
+        _torch.cuda.set_stream(before)
     if back >= 0:
         _torch.cuda.set_device(back)
 
@@ -450,23 +457,23 @@ def _current_stream(index):
     return raw(index) if raw is not None else _torch.cuda.current_stream(index).cuda_stream
 
 
-def _like(t, other):
+def _like(t, before):
     n = _torch.empty_like(t)
-    if other is not None:
-        n.record_stream(other)
+    if before is not None:
+        n.record_stream(before)
     return n
 
 
-def _new(t, shape, dtype, other):
+def _new(t, shape, dtype, before):
     n = t.new_empty(shape, dtype=dtype)
-    if other is not None:
-        n.record_stream(other)
+    if before is not None:
+        n.record_stream(before)
     return n
 
 
-def _workspace(who, t, nbytes, given, other):
+def _workspace(who, t, nbytes, given):
     if given is None:
-        return _new(t, (nbytes or 1,), _U8, other)
+        return _new(t, (nbytes or 1,), _U8, None)
     if given.dtype != _U8 or not given.is_contiguous() or given.device != t.device:
         _refuse(who, "the workspace is not a contiguous uint8 tensor on the inputs' device")
     return given
@@ -515,14 +522,14 @@ def cb_vocab_xent_fwd(h, w, labels, ignore=-100, workspace=None, stream=None):
     L = lib()
     x = _xent(who, h, w, labels, ignore)
     r = ctypes.byref(x)
-    handle, other, back = _begin(h, stream)
+    handle, before, back = _begin(h, stream)
     try:
-        loss, lse = _new(h, (x.k,), _F32, other), _new(h, (x.k, x.n), _F32, other)
-        ws = _workspace(who, h, L.cb_vocab_xent_workspace_bytes(r, 0), workspace, other)
+        loss, lse = _new(h, (x.k,), _F32, before), _new(h, (x.k, x.n), _F32, before)
+        ws = _workspace(who, h, L.cb_vocab_xent_workspace_bytes(r, 0), workspace)
         _check(who, L.cb_vocab_xent_fwd(r, loss.data_ptr(), lse.data_ptr(), ws.data_ptr(),
                                         ws.numel(), handle))
     finally:
-        _end(back)
+        _end(before, back)
     return loss, lse
 
 
@@ -538,17 +545,17 @@ def cb_vocab_xent_bwd(h, w, labels, lse, grad_scale=1.0, ignore=-100, dw=None, w
     _need(who, "lse", lse, (x.k, x.n), _F32, h.device)
     if dw is not None:
         _need(who, "dw", dw, (x.k, x.v, x.d), h.dtype, h.device, outer=True)
-    handle, other, back = _begin(h, stream)
+    handle, before, back = _begin(h, stream)
     try:
-        dh = _new(h, (x.k, x.n, x.d), h.dtype, other)
+        dh = _new(h, (x.k, x.n, x.d), h.dtype, before)
         if dw is None:
-            dw = _new(h, (x.k, x.v, x.d), h.dtype, other)
-        ws = _workspace(who, h, L.cb_vocab_xent_workspace_bytes(r, 1), workspace, other)
+            dw = _new(h, (x.k, x.v, x.d), h.dtype, before)
+        ws = _workspace(who, h, L.cb_vocab_xent_workspace_bytes(r, 1), workspace)
         _check(who, L.cb_vocab_xent_bwd(r, lse.data_ptr(), grad_scale, dh.data_ptr(),
                                         dw.data_ptr(), _outer(dw), ws.data_ptr(), ws.numel(),
                                         handle))
     finally:
-        _end(back)
+        _end(before, back)
     return dh, dw
 
 
@@ -592,15 +599,15 @@ def cb_gated_norm_fwd(x, block=None, gate=None, gate_rows=1, res_scale=1.0, post
     g = _norm(who, x, block, gate, gate_rows, res_scale, post, pre, eps)
     if keep and pre is None:
         _refuse(who, "keep without pre")
-    handle, other, back = _begin(x, stream)
+    handle, before, back = _begin(x, stream)
     try:
-        xo = _like(x, other) if block is not None else x
-        y = _like(x, other) if pre is not None else None
-        kept = _new_kept(x, other) if keep else None
+        xo = _like(x, before) if block is not None else x
+        y = _like(x, before) if pre is not None else None
+        kept = _new_kept(x, before) if keep else None
         _check(who, L.cb_gated_norm_fwd(ctypes.byref(g), x.data_ptr(), xo.data_ptr(), _ptr(y),
                                         kept.data.data_ptr() if keep else None, handle))
     finally:
-        _end(back)
+        _end(before, back)
     return (xo, y, kept) if keep else (xo, y)
 
 
@@ -628,25 +635,25 @@ def cb_gated_norm_bwd(x_out, dy=None, dres=None, block=None, gate=None, gate_row
             if of is None:
                 _refuse(who, f"{name} without its gamma")
             _need(who, name, t, (g.k, g.d), _F32, x_out.device, outer=True)
-    handle, other, back = _begin(x_out, stream)
+    handle, before, back = _begin(x_out, stream)
     try:
-        dx = _like(x_out, other)
+        dx = _like(x_out, before)
         dblock = dgate = None
         if block is not None:
-            dblock = _like(block, other)
+            dblock = _like(block, before)
         if gate is not None:
-            dgate = _like(gate, other)
+            dgate = _like(gate, before)
         if post is not None and dpost is None:
-            dpost = _new(post, (g.k, g.d), _F32, other)
+            dpost = _new(post, (g.k, g.d), _F32, before)
         if pre is not None and dpre is None:
-            dpre = _new(pre, (g.k, g.d), _F32, other)
-        ws = _workspace(who, x_out, L.cb_gated_norm_workspace_bytes(r), workspace, other)
+            dpre = _new(pre, (g.k, g.d), _F32, before)
+        ws = _workspace(who, x_out, L.cb_gated_norm_workspace_bytes(r), workspace)
         _check(who, L.cb_gated_norm_bwd(
             r, x_out.data_ptr(), _ptr(dy), _ptr(dres), dx.data_ptr(), _ptr(dblock), _ptr(dgate),
             _ptr(dpost), _outer(dpost) if dpost is not None else 0, _ptr(dpre),
             _outer(dpre) if dpre is not None else 0, ws.data_ptr(), ws.numel(), handle))
     finally:
-        _end(back)
+        _end(before, back)
     out = {"dx": dx, "dblock": dblock, "dgate": dgate, "dpost": dpost, "dpre": dpre}
     return {name: t for name, t in out.items() if t is not None}
 
@@ -660,12 +667,12 @@ class Kept:
         self.data, self.shape, self.dtype = data, tuple(shape), dtype
 
 
-def _new_kept(x, other):
+def _new_kept(x, before):
     k, n, d = x.shape
     nbytes = lib().cb_ckpt_bytes(k * n, d)
     if nbytes == 0:
         _refuse("cb_ckpt_bytes", f"{tuple(x.shape)} is out of range")
-    return Kept(_new(x, (nbytes,), _U8, other), x.shape, x.dtype)
+    return Kept(_new(x, (nbytes,), _U8, before), x.shape, x.dtype)
 
 
 def _check_kept(who, kept):
@@ -686,13 +693,13 @@ def cb_ckpt_pack(x, stream=None):
     if x.dim() != 3 or min(x.shape) < 1:
         _refuse(who, "x is [k, n, d], none of them 0")
     _need(who, "x", x, x.shape, x.dtype, x.device)
-    handle, other, back = _begin(x, stream)
+    handle, before, back = _begin(x, stream)
     try:
-        kept = _new_kept(x, other)
+        kept = _new_kept(x, before)
         _check(who, lib().cb_ckpt_pack(code, x.shape[0] * x.shape[1], x.shape[2], x.data_ptr(),
                                        kept.data.data_ptr(), handle))
     finally:
-        _end(back)
+        _end(before, back)
     return kept
 
 
@@ -701,13 +708,13 @@ def cb_ckpt_unpack(kept, stream=None):
     who = "cb_ckpt_unpack"
     code = _check_kept(who, kept)
     k, n, d = kept.shape
-    handle, other, back = _begin(kept.data, stream)
+    handle, before, back = _begin(kept.data, stream)
     try:
-        x = _new(kept.data, kept.shape, kept.dtype, other)
+        x = _new(kept.data, kept.shape, kept.dtype, before)
         _check(who, lib().cb_ckpt_unpack(code, k * n, d, kept.data.data_ptr(), x.data_ptr(),
                                          handle))
     finally:
-        _end(back)
+        _end(before, back)
     return x
 
 
@@ -725,14 +732,14 @@ def cb_ckpt_wgrad(kept, dy, dw=None, workspace=None, stream=None):
     if dw is not None:
         _need(who, "dw", dw, (k, out, d), kept.dtype, dy.device, outer=True)
     L = lib()
-    handle, other, back = _begin(dy, stream)
+    handle, before, back = _begin(dy, stream)
     try:
         if dw is None:
-            dw = _new(dy, (k, out, d), kept.dtype, other)
+            dw = _new(dy, (k, out, d), kept.dtype, before)
         need = L.cb_ckpt_wgrad_workspace_bytes(code, k, n, d, out, dy.data_ptr())
-        ws = _workspace(who, dy, need, workspace, other)
+        ws = _workspace(who, dy, need, workspace)
         _check(who, L.cb_ckpt_wgrad(code, k, n, d, out, kept.data.data_ptr(), dy.data_ptr(),
                                     dw.data_ptr(), _outer(dw), ws.data_ptr(), ws.numel(), handle))
     finally:
-        _end(back)
+        _end(before, back)
     return dw

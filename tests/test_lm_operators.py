@@ -872,3 +872,24 @@ def test_package_refuses_on_the_gpu():
         with pytest.raises(cb.CBError) as e:
             f()
         assert e.value.code == cb.CB_EINVAL, i
+
+
+def test_memory_of_a_given_stream():
+    """A call on another stream takes none of the blocks that were just freed on the current one."""
+    h, w, y = (v.cuda() for v in xent_inputs(2, 40, 64, 900, BF16, pad=0.2))
+    want = cb.cb_vocab_xent_fwd(h, w, y)
+    grads = cb.cb_vocab_xent_bwd(h, w, y, want[1])
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()  # the inputs are there for every stream
+    sizes = [v.numel() * v.element_size() for v in (*want, *grads)]
+    freed = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(2)]
+    spans = [(v.data_ptr(), v.data_ptr() + v.numel()) for v in freed]
+    del freed
+    loss, lse = cb.cb_vocab_xent_fwd(h, w, y, stream=s)
+    dh, dw = cb.cb_vocab_xent_bwd(h, w, y, lse, stream=s)
+    for v in (loss, lse, dh, dw):
+        at, end = v.data_ptr(), v.data_ptr() + v.numel() * v.element_size()
+        assert all(end <= a or b <= at for a, b in spans)
+    assert torch.cuda.current_stream().cuda_stream == torch.cuda.default_stream().cuda_stream
+    torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.equal(a, b) for a, b in zip((*want, *grads), (loss, lse, dh, dw)))
