@@ -423,24 +423,29 @@ def _outer(t):
     return t.stride(0) if t.shape[0] > 1 else t.numel()
 
 
-def _begin(t, stream):
+def _begin(stream, t, *more):
     """Makes the device of t current, and `stream` if one is given, so that new tensors
     are that stream's memory: a block of another stream's may have been freed while
-    work queued there still reads it.  Returns the handle of the call's stream, what
-    was torch's current stream (where results are used next, which the allocator has
-    to know) if it was another one or None, and the device to return to or -1."""
+    work queued there still reads it.  For the same reason t and the call's other
+    tensors (or None) are marked as used on that stream.  Returns the handle of the
+    call's stream, what was torch's current stream (where results are used next, which
+    the allocator has to know) if it was another one or None, and the device to return
+    to or -1."""
     cuda, index = _torch.cuda, t.get_device()
+    handle, before = _current_stream(index), None
+    if stream is not None and stream.cuda_stream != handle:
+        for used in (t, *more):
+            if used is not None:
+                used.record_stream(stream)
+        handle, before = stream.cuda_stream, cuda.current_stream(index)
     back = cuda.current_device()
     if back != index:
         cuda.set_device(index)
     else:
         back = -1
-    here = _current_stream(index)
-    if stream is None or stream.cuda_stream == here:
-        return here, None, back
-    before = cuda.current_stream(index)
-    cuda.set_stream(stream)
-    return stream.cuda_stream, before, back
+    if before is not None:
+        cuda.set_stream(stream)
+    return handle, before, back
 
 
 def _end(before, back):
@@ -471,12 +476,14 @@ def _new(t, shape, dtype, before):
     return n
 
 
-def _workspace(who, t, nbytes, given):
-    if given is None:
-        return _new(t, (nbytes or 1,), _U8, None)
-    if given.dtype != _U8 or not given.is_contiguous() or given.device != t.device:
+def _check_workspace(who, t, given):
+    if given is not None and (given.dtype != _U8 or not given.is_contiguous()
+                              or given.device != t.device):
         _refuse(who, "the workspace is not a contiguous uint8 tensor on the inputs' device")
-    return given
+
+
+def _workspace(t, nbytes, given):
+    return _new(t, (nbytes or 1,), _U8, None) if given is None else given
 
 
 def _check(who, rc):
@@ -522,10 +529,11 @@ def cb_vocab_xent_fwd(h, w, labels, ignore=-100, workspace=None, stream=None):
     L = lib()
     x = _xent(who, h, w, labels, ignore)
     r = ctypes.byref(x)
-    handle, before, back = _begin(h, stream)
+    _check_workspace(who, h, workspace)
+    handle, before, back = _begin(stream, h, w, labels, workspace)
     try:
         loss, lse = _new(h, (x.k,), _F32, before), _new(h, (x.k, x.n), _F32, before)
-        ws = _workspace(who, h, L.cb_vocab_xent_workspace_bytes(r, 0), workspace)
+        ws = _workspace(h, L.cb_vocab_xent_workspace_bytes(r, 0), workspace)
         _check(who, L.cb_vocab_xent_fwd(r, loss.data_ptr(), lse.data_ptr(), ws.data_ptr(),
                                         ws.numel(), handle))
     finally:
@@ -545,12 +553,13 @@ def cb_vocab_xent_bwd(h, w, labels, lse, grad_scale=1.0, ignore=-100, dw=None, w
     _need(who, "lse", lse, (x.k, x.n), _F32, h.device)
     if dw is not None:
         _need(who, "dw", dw, (x.k, x.v, x.d), h.dtype, h.device, outer=True)
-    handle, before, back = _begin(h, stream)
+    _check_workspace(who, h, workspace)
+    handle, before, back = _begin(stream, h, w, labels, lse, dw, workspace)
     try:
         dh = _new(h, (x.k, x.n, x.d), h.dtype, before)
         if dw is None:
             dw = _new(h, (x.k, x.v, x.d), h.dtype, before)
-        ws = _workspace(who, h, L.cb_vocab_xent_workspace_bytes(r, 1), workspace)
+        ws = _workspace(h, L.cb_vocab_xent_workspace_bytes(r, 1), workspace)
         _check(who, L.cb_vocab_xent_bwd(r, lse.data_ptr(), grad_scale, dh.data_ptr(),
                                         dw.data_ptr(), _outer(dw), ws.data_ptr(), ws.numel(),
                                         handle))
@@ -599,7 +608,7 @@ def cb_gated_norm_fwd(x, block=None, gate=None, gate_rows=1, res_scale=1.0, post
     g = _norm(who, x, block, gate, gate_rows, res_scale, post, pre, eps)
     if keep and pre is None:
         _refuse(who, "keep without pre")
-    handle, before, back = _begin(x, stream)
+    handle, before, back = _begin(stream, x, block, gate, post, pre)
     try:
         xo = _like(x, before) if block is not None else x
         y = _like(x, before) if pre is not None else None
@@ -635,7 +644,9 @@ def cb_gated_norm_bwd(x_out, dy=None, dres=None, block=None, gate=None, gate_row
             if of is None:
                 _refuse(who, f"{name} without its gamma")
             _need(who, name, t, (g.k, g.d), _F32, x_out.device, outer=True)
-    handle, before, back = _begin(x_out, stream)
+    _check_workspace(who, x_out, workspace)
+    handle, before, back = _begin(stream, x_out, dy, dres, block, gate, post, pre, dpost,
+                                  dpre, workspace)
     try:
         dx = _like(x_out, before)
         dblock = dgate = None
@@ -647,7 +658,7 @@ def cb_gated_norm_bwd(x_out, dy=None, dres=None, block=None, gate=None, gate_row
             dpost = _new(post, (g.k, g.d), _F32, before)
         if pre is not None and dpre is None:
             dpre = _new(pre, (g.k, g.d), _F32, before)
-        ws = _workspace(who, x_out, L.cb_gated_norm_workspace_bytes(r), workspace)
+        ws = _workspace(x_out, L.cb_gated_norm_workspace_bytes(r), workspace)
         _check(who, L.cb_gated_norm_bwd(
             r, x_out.data_ptr(), _ptr(dy), _ptr(dres), dx.data_ptr(), _ptr(dblock), _ptr(dgate),
             _ptr(dpost), _outer(dpost) if dpost is not None else 0, _ptr(dpre),
@@ -693,7 +704,7 @@ def cb_ckpt_pack(x, stream=None):
     if x.dim() != 3 or min(x.shape) < 1:
         _refuse(who, "x is [k, n, d], none of them 0")
     _need(who, "x", x, x.shape, x.dtype, x.device)
-    handle, before, back = _begin(x, stream)
+    handle, before, back = _begin(stream, x)
     try:
         kept = _new_kept(x, before)
         _check(who, lib().cb_ckpt_pack(code, x.shape[0] * x.shape[1], x.shape[2], x.data_ptr(),
@@ -708,7 +719,7 @@ def cb_ckpt_unpack(kept, stream=None):
     who = "cb_ckpt_unpack"
     code = _check_kept(who, kept)
     k, n, d = kept.shape
-    handle, before, back = _begin(kept.data, stream)
+    handle, before, back = _begin(stream, kept.data)
     try:
         x = _new(kept.data, kept.shape, kept.dtype, before)
         _check(who, lib().cb_ckpt_unpack(code, k * n, d, kept.data.data_ptr(), x.data_ptr(),
@@ -732,12 +743,13 @@ def cb_ckpt_wgrad(kept, dy, dw=None, workspace=None, stream=None):
     if dw is not None:
         _need(who, "dw", dw, (k, out, d), kept.dtype, dy.device, outer=True)
     L = lib()
-    handle, before, back = _begin(dy, stream)
+    _check_workspace(who, dy, workspace)
+    handle, before, back = _begin(stream, dy, kept.data, dw, workspace)
     try:
         if dw is None:
             dw = _new(dy, (k, out, d), kept.dtype, before)
         need = L.cb_ckpt_wgrad_workspace_bytes(code, k, n, d, out, dy.data_ptr())
-        ws = _workspace(who, dy, need, workspace)
+        ws = _workspace(dy, need, workspace)
         _check(who, L.cb_ckpt_wgrad(code, k, n, d, out, kept.data.data_ptr(), dy.data_ptr(),
                                     dw.data_ptr(), _outer(dw), ws.data_ptr(), ws.numel(), handle))
     finally:

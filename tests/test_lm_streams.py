@@ -74,6 +74,8 @@ class Tensor:
         return Tensor(self.cuda, shape, dtype, self.index)
 
     def record_stream(self, stream):
+        if not self.is_cuda:
+            raise NotImplementedError
         self.marked.append(stream.cuda_stream)
 
 
@@ -212,3 +214,26 @@ def test_device_of_the_inputs(name, fake):
     f(None)
     assert [(handle, device) for _, handle, device in library.launches] == [(77, 0), (0, 0)]
     assert cuda.device == 1 and cuda.streams[1].cuda_stream == 0 and cuda.streams[0].cuda_stream == 0
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_inputs_of_a_given_stream(name, fake):
+    """Inputs, given outputs and a given workspace are marked for the other stream: a caller who drops one after the
+    call does not have its memory taken while the work there still uses it."""
+    cuda, _ = fake
+    f, inputs = calls(cuda)[name]
+    f(Stream(77))
+    assert all(77 in t.marked for t in inputs)
+
+
+@pytest.mark.parametrize("what", ["type", "device", "host"])
+def test_a_refused_workspace_leaves_the_streams_as_they_were(what, fake):
+    cuda, library = fake
+    h, w, y = cuda.tensor((K, N, D)), cuda.tensor((K, V, D)), cuda.tensor((K, N), torch.int32)
+    ws = cuda.tensor((1 << 28,), torch.float32 if what == "type" else torch.uint8, 1 if what == "device" else 0)
+    if what == "host":
+        ws.is_cuda, ws.device = False, torch.device("cpu")
+    with pytest.raises(cb.CBError) as e:
+        cb.cb_vocab_xent_fwd(h, w, y, workspace=ws, stream=Stream(77))
+    assert e.value.code == cb.CB_EINVAL
+    assert cuda.current_stream().cuda_stream == 0 and cuda.device == 0 and not library.launches
