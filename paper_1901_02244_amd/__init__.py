@@ -423,7 +423,7 @@ def _outer(t):
     return t.stride(0) if t.shape[0] > 1 else t.numel()
 
 
-def _begin(stream, t, *more):
+def _begin(who, stream, t, *more):
     """Makes the device of t current, and `stream` if one is given, so that new tensors
     are that stream's memory: a block of another stream's may have been freed while
     work queued there still reads it.  For the same reason t and the call's other
@@ -432,6 +432,8 @@ def _begin(stream, t, *more):
     the allocator has to know) if it was another one or None, and the device to return
     to or -1."""
     cuda, index = _torch.cuda, t.get_device()
+    if stream is not None and stream.device_index != index:
+        _refuse(who, f"the stream is not one of {t.device}")
     handle, before = _current_stream(index), None
     if stream is not None and stream.cuda_stream != handle:
         for used in (t, *more):
@@ -530,7 +532,7 @@ def cb_vocab_xent_fwd(h, w, labels, ignore=-100, workspace=None, stream=None):
     x = _xent(who, h, w, labels, ignore)
     r = ctypes.byref(x)
     _check_workspace(who, h, workspace)
-    handle, before, back = _begin(stream, h, w, labels, workspace)
+    handle, before, back = _begin(who, stream, h, w, labels, workspace)
     try:
         loss, lse = _new(h, (x.k,), _F32, before), _new(h, (x.k, x.n), _F32, before)
         ws = _workspace(h, L.cb_vocab_xent_workspace_bytes(r, 0), workspace)
@@ -554,7 +556,7 @@ def cb_vocab_xent_bwd(h, w, labels, lse, grad_scale=1.0, ignore=-100, dw=None, w
     if dw is not None:
         _need(who, "dw", dw, (x.k, x.v, x.d), h.dtype, h.device, outer=True)
     _check_workspace(who, h, workspace)
-    handle, before, back = _begin(stream, h, w, labels, lse, dw, workspace)
+    handle, before, back = _begin(who, stream, h, w, labels, lse, dw, workspace)
     try:
         dh = _new(h, (x.k, x.n, x.d), h.dtype, before)
         if dw is None:
@@ -608,7 +610,7 @@ def cb_gated_norm_fwd(x, block=None, gate=None, gate_rows=1, res_scale=1.0, post
     g = _norm(who, x, block, gate, gate_rows, res_scale, post, pre, eps)
     if keep and pre is None:
         _refuse(who, "keep without pre")
-    handle, before, back = _begin(stream, x, block, gate, post, pre)
+    handle, before, back = _begin(who, stream, x, block, gate, post, pre)
     try:
         xo = _like(x, before) if block is not None else x
         y = _like(x, before) if pre is not None else None
@@ -645,7 +647,7 @@ def cb_gated_norm_bwd(x_out, dy=None, dres=None, block=None, gate=None, gate_row
                 _refuse(who, f"{name} without its gamma")
             _need(who, name, t, (g.k, g.d), _F32, x_out.device, outer=True)
     _check_workspace(who, x_out, workspace)
-    handle, before, back = _begin(stream, x_out, dy, dres, block, gate, post, pre, dpost,
+    handle, before, back = _begin(who, stream, x_out, dy, dres, block, gate, post, pre, dpost,
                                   dpre, workspace)
     try:
         dx = _like(x_out, before)
@@ -704,7 +706,7 @@ def cb_ckpt_pack(x, stream=None):
     if x.dim() != 3 or min(x.shape) < 1:
         _refuse(who, "x is [k, n, d], none of them 0")
     _need(who, "x", x, x.shape, x.dtype, x.device)
-    handle, before, back = _begin(stream, x)
+    handle, before, back = _begin(who, stream, x)
     try:
         kept = _new_kept(x, before)
         _check(who, lib().cb_ckpt_pack(code, x.shape[0] * x.shape[1], x.shape[2], x.data_ptr(),
@@ -719,7 +721,7 @@ def cb_ckpt_unpack(kept, stream=None):
     who = "cb_ckpt_unpack"
     code = _check_kept(who, kept)
     k, n, d = kept.shape
-    handle, before, back = _begin(stream, kept.data)
+    handle, before, back = _begin(who, stream, kept.data)
     try:
         x = _new(kept.data, kept.shape, kept.dtype, before)
         _check(who, lib().cb_ckpt_unpack(code, k * n, d, kept.data.data_ptr(), x.data_ptr(),
@@ -744,7 +746,7 @@ def cb_ckpt_wgrad(kept, dy, dw=None, workspace=None, stream=None):
         _need(who, "dw", dw, (k, out, d), kept.dtype, dy.device, outer=True)
     L = lib()
     _check_workspace(who, dy, workspace)
-    handle, before, back = _begin(stream, dy, kept.data, dw, workspace)
+    handle, before, back = _begin(who, stream, dy, kept.data, dw, workspace)
     try:
         if dw is None:
             dw = _new(dy, (k, out, d), kept.dtype, before)

@@ -237,3 +237,16 @@ def test_a_refused_workspace_leaves_the_streams_as_they_were(what, fake):
         cb.cb_vocab_xent_fwd(h, w, y, workspace=ws, stream=Stream(77))
     assert e.value.code == cb.CB_EINVAL
     assert cuda.current_stream().cuda_stream == 0 and cuda.device == 0 and not library.launches
+
+
+@pytest.mark.parametrize("handle", [0, 77])
+@pytest.mark.parametrize("name", NAMES)
+def test_a_stream_of_another_device_is_refused(name, handle, fake):
+    """The default streams of all devices have the handle 0: the device tells them apart."""
+    cuda, library = fake
+    f, inputs = calls(cuda)[name]
+    with pytest.raises(cb.CBError) as e:
+        f(Stream(handle, 1))
+    assert e.value.code == cb.CB_EINVAL and "stream" in str(e.value)
+    assert not library.launches and not any(t.marked for t in inputs)
+    assert cuda.device == 0 and [s.cuda_stream for s in cuda.streams] == [0, 0]
