@@ -401,6 +401,11 @@ def _type_code(who, dtype):
     return code
 
 
+# Sizes are 32-bit numbers in the library, and ctypes would cut larger ones off:
+# (a | b | c) >> 31 is 0 where none of them is negative or takes more.
+_PAST = "a size or label past 32 bits"
+
+
 def _need(who, name, t, shape, dtype, device, outer=False):
     """Checks one tensor: its shape, type, device, and that it is contiguous (with
     `outer`: apart from the stride of its first dimension)."""
@@ -503,6 +508,8 @@ def _xent(who, h, w, labels, ignore):
         _refuse(who, "h is [k, n, d] and w [k, v, d]")
     k, n, d = h.shape
     v = w.shape[1]
+    if (k | n | d | v) >> 31 or not -2**31 <= ignore < 2**31:
+        _refuse(who, _PAST)
     if not h.is_cuda:
         _refuse(who, "h is not on a GPU")
     if min(k, n, d, v) < 1:
@@ -576,6 +583,8 @@ def _norm(who, x, block, gate, gate_rows, res_scale, post, pre, eps):
     if len(shape) != 3 or min(shape) < 1:
         _refuse(who, "x is [k, n, d], none of them 0")
     k, n, d = shape
+    if (k | n | d) >> 31:
+        _refuse(who, _PAST)
     _need(who, "x", x, shape, dtype, dev)
     if block is not None:
         _need(who, "block", block, shape, dtype, dev)
@@ -691,7 +700,10 @@ def _new_kept(x, before):
 def _check_kept(who, kept):
     """The type code of a Kept whose buffer is as long as its shape says."""
     code = _type_code(who, kept.dtype)
-    need = lib().cb_ckpt_bytes(kept.shape[0] * kept.shape[1], kept.shape[2])
+    k, n, d = kept.shape
+    if (k | n | d) >> 31:
+        _refuse(who, _PAST)
+    need = lib().cb_ckpt_bytes(k * n, d)
     b = kept.data
     if not b.is_cuda or b.dtype != _U8 or not b.is_contiguous() or need == 0 or b.numel() < need:
         _refuse(who, f"the kept buffer is not {need} bytes on a GPU")
@@ -705,12 +717,14 @@ def cb_ckpt_pack(x, stream=None):
     code = _type_code(who, x.dtype)
     if x.dim() != 3 or min(x.shape) < 1:
         _refuse(who, "x is [k, n, d], none of them 0")
+    k, n, d = x.shape
+    if (k | n | d) >> 31:
+        _refuse(who, _PAST)
     _need(who, "x", x, x.shape, x.dtype, x.device)
     handle, before, back = _begin(who, stream, x)
     try:
         kept = _new_kept(x, before)
-        _check(who, lib().cb_ckpt_pack(code, x.shape[0] * x.shape[1], x.shape[2], x.data_ptr(),
-                                       kept.data.data_ptr(), handle))
+        _check(who, lib().cb_ckpt_pack(code, k * n, d, x.data_ptr(), kept.data.data_ptr(), handle))
     finally:
         _end(before, back)
     return kept
@@ -736,11 +750,13 @@ def cb_ckpt_wgrad(kept, dy, dw=None, workspace=None, stream=None):
     bits: dw [k, out, d] = dy^T x for dy [k, n, out] of the same type.  dw may be
     given, for instance as a view of a flat gradient vector; it is overwritten."""
     who = "cb_ckpt_wgrad"
-    code = _check_kept(who, kept)
-    k, n, d = kept.shape
     if dy.dim() != 3 or dy.shape[2] < 1:
         _refuse(who, "dy is [k, n, out]")
     out = dy.shape[2]
+    if out >> 31:
+        _refuse(who, _PAST)
+    code = _check_kept(who, kept)
+    k, n, d = kept.shape
     _need(who, "dy", dy, (k, n, out), kept.dtype, kept.data.device)
     if dw is not None:
         _need(who, "dw", dw, (k, out, d), kept.dtype, dy.device, outer=True)

@@ -174,3 +174,34 @@ def test_package_refuses_cpu_and_misshapen_tensors():
         with pytest.raises(cb.CBError) as e:
             f()
         assert e.value.code == cb.CB_EINVAL
+
+
+def test_package_refuses_what_32_bits_do_not_hold():
+    """The library's sizes and labels are 32-bit: larger ones are refused, not taken modulo 2^32."""
+    big = 2 ** 32 + 4
+
+    def m(*shape, t=torch.float32):
+        return torch.empty(*shape, dtype=t, device="meta")
+
+    i, z = torch.int32, m(1, 4, 8)
+    kept = cb.Kept(torch.zeros(1 << 10, dtype=torch.uint8), (1, 4, 8), torch.float32)
+    bad = [
+        lambda: cb.cb_vocab_xent_fwd(z, m(1, 9, 8), m(1, 4, t=i), ignore=2 ** 32 - 100),
+        lambda: cb.cb_vocab_xent_fwd(z, m(1, 9, 8), m(1, 4, t=i), ignore=-2 ** 31 - 1),
+        lambda: cb.cb_vocab_xent_bwd(z, m(1, 9, 8), m(1, 4, t=i), m(1, 4), ignore=2 ** 31),
+        lambda: cb.cb_vocab_xent_fwd(m(1, big, 1), m(1, 9, 1), m(1, big, t=i)),
+        lambda: cb.cb_vocab_xent_fwd(m(1, 4, 1), m(1, big, 1), m(1, 4, t=i)),
+        lambda: cb.cb_vocab_xent_fwd(m(1, 4, big), m(1, 9, big), m(1, 4, t=i)),
+        lambda: cb.cb_vocab_xent_fwd(m(big, 1, 1), m(big, 1, 1), m(big, 1, t=i)),
+        lambda: cb.cb_gated_norm_fwd(m(1, big, 8), pre=m(1, 8)),
+        lambda: cb.cb_gated_norm_fwd(m(1, 4, big), pre=m(1, big)),
+        lambda: cb.cb_gated_norm_bwd(m(1, big, 8), dy=m(1, big, 8), pre=m(1, 8)),
+        lambda: cb.cb_ckpt_pack(m(1, 4, big)),
+        lambda: cb.cb_ckpt_unpack(cb.Kept(kept.data, (1, 4, big), torch.float32)),
+        lambda: cb.cb_ckpt_wgrad(cb.Kept(kept.data, (1, big, 8), torch.float32), m(1, big, 3)),
+        lambda: cb.cb_ckpt_wgrad(kept, m(1, 4, big)),
+    ]
+    for n, f in enumerate(bad):
+        with pytest.raises(cb.CBError, match="32 bits") as e:
+            f()
+        assert e.value.code == cb.CB_EINVAL, n
