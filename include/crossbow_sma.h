@@ -538,7 +538,8 @@ int cb_profile_clear(cb_ctx* c);
 /* Message for the last error on this context ("" if none); valid until the
  * next call on it.  A NULL context gives the last failure of a call made
  * without one (cb_create, cb_test_conv_static, the language-model
- * operators). */
+ * operators), whichever thread made it; that message is valid until the same
+ * thread asks again. */
 const char* cb_last_error(const cb_ctx* c);
 
 /* Frees the context's host-side state; the caller then frees the workspace. */

@@ -13,6 +13,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <mutex>
 #include <string>
 #include <vector>
 
@@ -569,17 +570,22 @@ struct cb_ctx {
 
 namespace {
 
-thread_local std::string g_create_error;
+// The last failure of a call without a context, of any thread.
+std::mutex g_noted_lock;
+std::string g_noted;
 
 }  // namespace
 
-void cbk::note_error(const std::string& msg) { g_create_error = msg; }
+void cbk::note_error(const std::string& msg) {
+  std::lock_guard<std::mutex> hold(g_noted_lock);
+  g_noted = msg;
+}
 
 namespace {
 
 int fail(cb_ctx* c, int code, const std::string& msg) {
   if (c) c->err = msg;
-  else g_create_error = msg;
+  else cbk::note_error(msg);
   return code;
 }
 
@@ -1226,7 +1232,7 @@ int cb_create(const cb_model* m, int k, int b, float alpha, float lr, float mome
   int rc = CB_OK;
   auto dev = [&](hipError_t e, const char* what) {
     if (e != hipSuccess && rc == CB_OK) {
-      g_create_error = std::string(what) + ": " + hipGetErrorString(e);
+      cbk::note_error(std::string(what) + ": " + hipGetErrorString(e));
       rc = CB_EDEVICE;
     }
   };
@@ -1498,7 +1504,16 @@ int cb_profile_clear(cb_ctx* c) {
 }
 
 const char* cb_last_error(const cb_ctx* c) {
-  return c ? c->err.c_str() : g_create_error.c_str();
+  if (c) return c->err.c_str();
+  // this thread's copy: another thread's failure may replace the original
+  thread_local std::string copy;
+  try {
+    std::lock_guard<std::mutex> hold(g_noted_lock);
+    copy = g_noted;
+  } catch (...) {
+    return "out of host memory";
+  }
+  return copy.c_str();
 }
 
 void cb_destroy(cb_ctx* c) { delete c; }

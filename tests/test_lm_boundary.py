@@ -205,3 +205,47 @@ def test_package_refuses_what_32_bits_do_not_hold():
         with pytest.raises(cb.CBError, match="32 bits") as e:
             f()
         assert e.value.code == cb.CB_EINVAL, n
+
+
+def test_last_error_of_another_thread():
+    """Without a context there is one last failure, whichever thread made the call: one thread may create and another
+    report."""
+    import threading
+
+    L = cb.lib()
+    m = cb.model("lenet5", 1, 28, 28, 10)
+    out = ctypes.c_void_p()
+
+    def create():
+        P = cb.cb_num_params(m)
+        w0 = (ctypes.c_float * P)()
+        assert L.cb_create(ctypes.byref(m), 2, 4, 0.5, 0.01, 0.9, w0, P, A, 256, None,
+                           ctypes.byref(out)) == cb.CB_ENOMEM
+
+    assert L.cb_vocab_xent_fwd(None, A, A, A, BIG, None) == cb.CB_EINVAL and "cb_vocab_xent_fwd" in _err()
+    t = threading.Thread(target=create)
+    t.start()
+    t.join()
+    assert "workspace" in _err() and "cb_vocab_xent_fwd" not in _err()
+
+
+def test_last_error_of_many_threads():
+    """Threads that fail and read at the same time: every message is a whole one."""
+    import threading
+
+    L, seen = cb.lib(), [set() for _ in range(8)]
+
+    def work(i):
+        bad = [xent(n=0), xent(ldh=63), xent(h=None), xent(pstride=3)][i % 4]
+        for _ in range(2000):
+            L.cb_vocab_xent_fwd(ctypes.byref(bad), A, A, A, BIG, None)
+            L.cb_vocab_xent_bwd(ctypes.byref(bad), A, 1.0, A, A, 64000, A, BIG, None)
+            seen[i].add(_err())
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(8)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    why = ["k or n out of range", "ldh is less than d", "h, w or labels NULL or misaligned", "pstride is less than v * d"]
+    assert set().union(*seen) <= {f"cb_vocab_xent_{f}: {w}" for f in ("fwd", "bwd") for w in why}
