@@ -362,7 +362,7 @@ struct Layout {
   int full, tail, splits, span;
   int64_t ldx, ldy;
   bool copy_dy;
-  size_t x, dy, part, total;
+  size_t x, dy, part, total;  // total 0: a launch would not hold its workgroups
 };
 
 Layout layout(const KeptGradArgs& a) {
@@ -397,7 +397,7 @@ Layout layout(const KeptGradArgs& a) {
   l.x = l.big ? take((int64_t)a.k * a.n * l.ldx * sz) : 0;
   l.part = l.tail ? take(l.splits * l.tail * side * side * 4) : 0;
   l.dy = l.copy_dy ? take((int64_t)a.k * a.n * l.ldy * sz) : 0;
-  l.total = std::max<size_t>(at, 256);
+  l.total = launch_holds(full + l.splits * tail, l.big ? 512 : 256) ? std::max<size_t>(at, 256) : 0;
   return l;
 }
 
@@ -432,7 +432,8 @@ hipError_t launch_grad(const GradArgs& g, hipStream_t s) {
 template <class T>
 hipError_t grad(const KeptGradArgs& a, hipStream_t s) {
   static_assert(Big<_Float16>::BP == 256 && Big<_Float16>::BQ == 256 && Mid<T>::BP == 128 &&
-                Mid<T>::BQ == 128, "as layout() counts them");
+                Mid<T>::BQ == 128 && Big<_Float16>::THREADS == 512 && Mid<T>::THREADS == 256,
+                "as layout() counts them");
   const Layout l = layout(a);
   char* ws = (char*)a.ws;
   GradArgs g;

@@ -31,7 +31,7 @@ struct XentArgs {
   int64_t dstride;
   void* ws;
 };
-size_t xent_ws_bytes(const XentArgs& a, bool backward);
+size_t xent_ws_bytes(const XentArgs& a, bool backward);  // 0: too large for a launch
 hipError_t xent_fwd(const XentArgs& a, hipStream_t s);
 hipError_t xent_bwd(const XentArgs& a, hipStream_t s);
 
@@ -73,7 +73,7 @@ struct KeptGradArgs {
   int64_t dstride;
   void* ws;
 };
-size_t kept_grad_ws_bytes(const KeptGradArgs& a);
+size_t kept_grad_ws_bytes(const KeptGradArgs& a);  // 0: too large for a launch
 hipError_t kept_grad(const KeptGradArgs& a, hipStream_t s);
 
 }  // namespace cbk

@@ -19,6 +19,11 @@ int refuse(const char* who, const char* why, int code = CB_EINVAL) {
   note_error(std::string(who) + ": " + why);
   return code;
 }
+// A workspace of `given` bytes where `need` are needed (0: more than a launch holds).
+int short_of(const char* who, size_t need, size_t given) {
+  if (need == 0) return refuse(who, "more workgroups than a launch holds");
+  return given < need ? refuse(who, "workspace too small", CB_ENOMEM) : CB_OK;
+}
 int done(const char* who, hipError_t e) {
   if (e == hipSuccess) return CB_OK;
   note_error(std::string(who) + ": " + hipGetErrorString(e));
@@ -154,7 +159,7 @@ int cb_vocab_xent_fwd(const cb_vocab_xent* x, float* loss, float* lse, void* wor
     if (!at(loss, 4) || !at(lse, 4)) return refuse(me, "loss or lse NULL or misaligned");
     if (!at(workspace_dev, 256)) return refuse(me, "workspace NULL or not on 256 bytes");
     XentArgs a = xent_args(x);
-    if (ws_bytes < xent_ws_bytes(a, false)) return refuse(me, "workspace too small", CB_ENOMEM);
+    if (int rc = short_of(me, xent_ws_bytes(a, false), ws_bytes)) return rc;
     a.loss = loss;
     a.lse = lse;
     a.ws = workspace_dev;
@@ -176,7 +181,7 @@ int cb_vocab_xent_bwd(const cb_vocab_xent* x, const float* lse, float grad_scale
       return refuse(me, "dstride is less than v * d");
     if (!at(workspace_dev, 256)) return refuse(me, "workspace NULL or not on 256 bytes");
     XentArgs a = xent_args(x);
-    if (ws_bytes < xent_ws_bytes(a, true)) return refuse(me, "workspace too small", CB_ENOMEM);
+    if (int rc = short_of(me, xent_ws_bytes(a, true), ws_bytes)) return rc;
     a.lse = const_cast<float*>(lse);
     a.grad_scale = grad_scale;
     a.dh = dh;
@@ -233,8 +238,8 @@ int cb_gated_norm_bwd(const cb_gated_norm* g, const void* x_out, const void* dy,
       return refuse(me, "dpost_stride or dpre_stride is less than d");
     if (!at(workspace_dev, 256)) return refuse(me, "workspace NULL or not on 256 bytes");
     NormArgs a = norm_args(g);
-    if (ws_bytes < norm_ws_bytes(a.type, a.k, a.n, a.d, a.gate_rows))
-      return refuse(me, "workspace too small", CB_ENOMEM);
+    const size_t need = norm_ws_bytes(a.type, a.k, a.n, a.d, a.gate_rows);
+    if (int rc = short_of(me, need, ws_bytes)) return rc;
     a.x = g->pre ? x_out : nullptr;
     a.dy = dy;
     a.dres = dres;
@@ -288,7 +293,7 @@ int cb_ckpt_wgrad(int type, int k, int n, int d, int out, const void* kept, cons
     if (k > 1 && dstride < (int64_t)out * d) return refuse(me, "dstride is less than out * d");
     if (!at(workspace_dev, 256)) return refuse(me, "workspace NULL or not on 256 bytes");
     KeptGradArgs a = wgrad_args(type, k, n, d, out, dy);
-    if (ws_bytes < kept_grad_ws_bytes(a)) return refuse(me, "workspace too small", CB_ENOMEM);
+    if (int rc = short_of(me, kept_grad_ws_bytes(a), ws_bytes)) return rc;
     a.kept = kept;
     a.dw = dw;
     a.dstride = dstride;

@@ -470,6 +470,12 @@ using MidTile = Tile<T, PC, QC, 128, 128, 2, 2>;
 template <class T, bool PC, bool QC>
 using ThinTile = Tile<T, PC, QC, 256, THIN_Q, 4, 1>;
 
+// Whether the first axis of a grid holds these workgroups: its threads are a
+// 32-bit number.
+inline bool launch_holds(int64_t workgroups, int threads) {
+  return workgroups <= UINT32_MAX / threads;
+}
+
 // Launches KERNEL with LDS bytes of dynamic LDS.  More than 64 KB has to be
 // asked for, once per kernel and device.
 template <int LDS, auto KERNEL, class A>

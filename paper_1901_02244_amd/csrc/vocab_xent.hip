@@ -59,6 +59,7 @@ constexpr double MID_COST = 1.3;
 int64_t tiles(int64_t a, int64_t b, int ba, int bb) { return up(a, ba) / ba * (up(b, bb) / bb); }
 constexpr int bp_of(int shape) { return shape == MID ? 128 : 256; }
 constexpr int bq_of(int shape) { return shape == BIG ? 256 : shape == MID ? 128 : THIN_Q; }
+constexpr int threads_of(int shape) { return shape == BIG ? 512 : 256; }
 int64_t tiles_of(int shape, int k, int64_t p, int64_t q) {
   return k * tiles(p, q, bp_of(shape), bq_of(shape));
 }
@@ -100,11 +101,27 @@ struct Layout {
   Plan logits, dh, dw;
   bool copy_w;
   size_t cnt, chunks, pos, row, lab, hc, wc, part, plog, rloss, means, g, lsum, dhsum, dwsum,
-      total;
+      total;      // 0: a launch would not hold its workgroups
 };
 
 Plan plan_logits(int type, int k, int n, int d, int v) {
   return plan(type, k, v, n, d, true, false);
+}
+
+// dW of a piece of vn words: the first one's splits, if it has any, which the
+// workspace has sums for.
+Plan plan_dw(const XentArgs& a, const Layout& l, int64_t vn) {
+  return l.dw.splits > 1 ? l.dw : plan(a.type, a.k, a.d, vn, 0, false, false);
+}
+
+// Whether a launch of both gradients holds its workgroups, as launch_grads()
+// counts them.
+bool grads_fit(const XentArgs& a, Plan h, Plan w, int64_t vn) {
+  const int64_t hw = a.k * tiles(a.d, a.n, bp_of(h.shape), bq_of(h.shape)) * h.splits;
+  const int64_t ww = a.k * tiles(a.d, vn, bp_of(w.shape), bq_of(w.shape)) * w.splits;
+  if ((h.shape == BIG) != (w.shape == BIG))
+    return launch_holds(hw, threads_of(h.shape)) && launch_holds(ww, threads_of(w.shape));
+  return launch_holds(up(hw, NXCD) + ww, threads_of(h.shape));
 }
 
 Layout layout(const XentArgs& a, bool backward) {
@@ -162,7 +179,20 @@ Layout layout(const XentArgs& a, bool backward) {
     l.rloss = take((int64_t)k * n * 4);
     l.means = n > MANY ? take(up(n, CHUNK) / CHUNK * k * 16) : 0;
   }
-  l.total = at;
+  // the gathering of the rows, the logits, and for whole pieces and the last
+  // one logits and gradients; the other launches have a bounded grid
+  bool fits = n <= MANY || launch_holds(up(n, 32) / 32, 256);
+  if (!backward) {
+    const int64_t words = l.logits.shape == THIN ? (int64_t)l.parts * 256 : v;
+    fits &= launch_holds(tiles_of(l.logits.shape, 1, words, n), threads_of(l.logits.shape));
+  } else {
+    for (const int64_t vn : {std::min(l.piece, v), (v - 1) % l.piece + 1}) {
+      const int shape = plan_logits(a.type, k, n, d, (int)vn).shape;
+      fits &= launch_holds(tiles_of(shape, 1, vn, n), threads_of(shape)) &&
+              grads_fit(a, l.dh, plan_dw(a, l, vn), vn);
+    }
+  }
+  l.total = fits ? at : 0;
   return l;
 }
 
@@ -903,6 +933,8 @@ hipError_t launch_logits(const LogitArgs& a, Plan p, int k, int n, hipStream_t s
   using Big = BigTile<T, false, false>;
   using Mid = MidTile<T, false, false>;
   using Thin = ThinTile<T, false, false>;
+  static_assert(Big::THREADS == threads_of(BIG) && Mid::THREADS == threads_of(MID) &&
+                Thin::THREADS == threads_of(THIN));
   static_assert(Big::BP == bp_of(BIG) && Big::BQ == bq_of(BIG) && Mid::BP == bp_of(MID) &&
                 Mid::BQ == bq_of(MID) && Thin::BP == bp_of(THIN) && Thin::BQ == bq_of(THIN));
   if constexpr (sizeof(T) == 2 && MODE != SUMS)
@@ -1150,8 +1182,7 @@ hipError_t backward(const XentArgs& a, hipStream_t s) {
     dh.pieces = dw.pieces = g.pieces;
     dw.vn = vn;
     dw.split_stride = (int64_t)a.k * vn * l.dp;
-    const Plan pw = l.dw.splits > 1 ? l.dw : plan(a.type, a.k, a.d, vn, 0, false, false);
-    if (hipError_t e = launch_grads<T>(dh, l.dh, dw, pw, a.k, s)) return e;
+    if (hipError_t e = launch_grads<T>(dh, l.dh, dw, plan_dw(a, l, vn), a.k, s)) return e;
     if (dw.sums) {
       const int64_t blocks = ((int64_t)vn * ((a.d + 3) / 4) + 255) / 256;
       klaunch(xent_dw_join<T>, dim3((unsigned)std::min<int64_t>(blocks, 2048), a.k), dim3(256), 0,

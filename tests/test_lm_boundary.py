@@ -249,3 +249,44 @@ def test_last_error_of_many_threads():
         t.join()
     why = ["k or n out of range", "ldh is less than d", "h, w or labels NULL or misaligned", "pstride is less than v * d"]
     assert set().union(*seen) <= {f"cb_vocab_xent_{f}: {w}" for f in ("fwd", "bwd") for w in why}
+
+
+# (description, forward fits, backward fits): a launch has fewer than 2^32 threads along its grid's first axis
+XENT_GRIDS = [
+    (dict(type=0, k=1, n=1 << 19, v=1 << 19), False, True),  # 2^24 tiles of 128 x 128, 256 threads each
+    (dict(type=0, k=1, n=(1 << 19) - 128, v=1 << 19), True, True),
+    (dict(type=2, k=1, n=1 << 20, v=1 << 19), False, True),  # 2^23 tiles of 256 x 256, 512 threads each
+    (dict(type=2, k=1, n=(1 << 20) - 256, v=1 << 19), True, True),
+    (dict(k=1, n=1 << 29, v=10), False, False),  # 32 rows a workgroup of 256
+    (dict(k=1, n=(1 << 29) - 32, v=10), True, True),
+    (dict(type=0, k=1, n=1 << 26, v=5000), False, False),  # 32 tiles of the piece's 4096 words, 2^19 of its rows
+    (dict(type=0, k=1, n=(1 << 26) - 2048, v=4096), True, True),
+    (dict(k=65535, n=1, d=1 << 20, ldh=1 << 20, v=1, pstride=1 << 20), True, False),  # 2^13 columns' tiles of dW
+    # 2^12 tiles of dh and 2^13 of dW a learner, in one launch: 2^24 / 12,288 is 1365
+    (dict(k=1366, n=1, d=1 << 20, ldh=1 << 20, v=1, pstride=1 << 20), True, False),
+    (dict(k=1365, n=1, d=1 << 20, ldh=1 << 20, v=1, pstride=1 << 20), True, True),
+]
+
+
+@pytest.mark.parametrize("kw, forward, backward", XENT_GRIDS, ids=str)
+def test_xent_refuses_what_a_launch_does_not_hold(kw, forward, backward):
+    """Before anything has run, and not by a launch that fails behind others."""
+    L, x = cb.lib(), xent(**kw)
+    r = ctypes.byref(x)
+    assert (L.cb_vocab_xent_workspace_bytes(r, 0) > 0) == forward
+    assert (L.cb_vocab_xent_workspace_bytes(r, 1) > 0) == backward
+    if not forward:
+        assert L.cb_vocab_xent_fwd(r, A, A, A, BIG, None) == cb.CB_EINVAL and "launch" in _err()
+    if not backward:
+        assert L.cb_vocab_xent_bwd(r, A, 1.0, A, A, x.pstride, A, BIG, None) == cb.CB_EINVAL and "launch" in _err()
+
+
+def test_ckpt_wgrad_refuses_what_a_launch_does_not_hold():
+    L = cb.lib()
+    for size, fits in (((0, 2048, 1, 1 << 20, 1), False), ((0, 2047, 1, 1 << 20, 1), True),
+                       ((2, 65535, 1, 1 << 20, 1 << 20), False), ((2, 4096, 1, 1 << 20, 1), False),
+                       ((2, 2040, 1, 1 << 20, 1), True)):
+        assert (L.cb_ckpt_wgrad_workspace_bytes(*size, A) > 0) == fits, size
+        if not fits:
+            stride = size[3] * size[4]
+            assert L.cb_ckpt_wgrad(*size, A, A, A, stride, A, BIG, None) == cb.CB_EINVAL and "launch" in _err()
