@@ -290,3 +290,34 @@ def test_ckpt_wgrad_refuses_what_a_launch_does_not_hold():
         if not fits:
             stride = size[3] * size[4]
             assert L.cb_ckpt_wgrad(*size, A, A, A, stride, A, BIG, None) == cb.CB_EINVAL and "launch" in _err()
+
+
+def test_xent_workspace_of_a_piece():
+    """The backward's workspace is its piece of 128 MB, the gathered rows, fp32 sums of dh and a few numbers a row."""
+    L = cb.lib()
+
+    def one(**kw):
+        return L.cb_vocab_xent_workspace_bytes(ctypes.byref(xent(k=1, n=8192, d=4096, ldh=4096, **kw)), 1)
+
+    assert (1 << 27) < one(v=128000) <= (1 << 27) + 8192 * 4096 * (2 + 4) + 8192 * 12 + 16 * 256
+    assert one(v=128000) == one(v=64000)
+
+
+SHARED = [(512, 4096, 2048), (128, 1 << 20, 100), (1, 1 << 16, 1), (20, 1600, 40), (300, 20000, 5000), (64, 8192, 30000),
+          (40000, 16384, 100), (33, 1 << 20, 256), (129, 1 << 18, 129)]
+
+
+@pytest.mark.parametrize("type", [0, 1, 2])
+@pytest.mark.parametrize("k", [1, 3])
+@pytest.mark.parametrize("size", SHARED, ids=str)
+def test_xent_workspace_of_shared_logits(size, k, type):
+    """Where few tiles share long sums the workspace also holds the shares' logits: 64 MB at the most."""
+    n, d, v = size
+    x = xent(type=type, k=k, n=n, d=d, ldh=d, v=v, pstride=d * v)
+    got = cb.lib().cb_vocab_xent_workspace_bytes(ctypes.byref(x), 0)
+    bytes_of = 4 if type == 0 else 2
+    cap, dp = -(-n // 64) * 64, -(-d * bytes_of // 128) * 128
+    rows = k * cap * dp + k * n * 8 + k * cap * 12 + 12 * 256  # the gathered rows, and a few numbers each
+    copy = 0 if d * bytes_of % 16 == 0 else k * v * dp + 256
+    parts = k * cap * 8 * -(-v // 16)  # a pair for a tile's words, 16 at the least
+    assert 0 < got <= rows + copy + parts + (64 << 20)

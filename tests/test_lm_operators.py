@@ -371,6 +371,24 @@ def test_norm_parts(parts, t):
 
 
 @pytest.mark.parametrize("t", TYPES, ids=str)
+@pytest.mark.parametrize("post", [0, 1])
+def test_norm_without_a_gradient(post, t):
+    """Without the norm before the next block and without a gradient of the stream there is nothing to go back: the
+    forward runs, the backward is refused."""
+    i, dy, dres = norm_inputs(2, 13, 72, 4, t, post, False, True)
+    g = on(i)
+    x = g.pop("x")
+    xo, y = cb.cb_gated_norm_fwd(x, **g, gate_rows=4, res_scale=0.5)
+    assert y is None
+    for j in range(2):
+        a = on(i, j)
+        close(f"x[{j}]", xo[j], ref.norm_fwd(a["x"], a["block"], a["gate"], 4, 0.5, a["post"], None, 1e-5)["x"])
+    with pytest.raises(cb.CBError) as e:
+        cb.cb_gated_norm_bwd(xo, **g, gate_rows=4, res_scale=0.5)
+    assert e.value.code == cb.CB_EINVAL
+
+
+@pytest.mark.parametrize("t", TYPES, ids=str)
 def test_norm_rows_of_zeros_and_nan(t):
     """A row of zeros has a finite norm; a row with a NaN spoils no other row."""
     i, dy, dres = norm_inputs(1, 6, 96, 1, t)
@@ -671,6 +689,22 @@ def test_ckpt_wgrad_of_the_largest_values(size, t):
         close(f"dw[{j}]", dw[j], ref.wgrad(values[j], dy[j])["dw"])
 
 
+@pytest.mark.parametrize("t", [F16, BF16], ids=str)
+@pytest.mark.parametrize("size", [(2, 40, 96, 40), (1, 130, 4104, 4100)], ids=str)
+def test_ckpt_wgrad_of_the_smallest_values(size, t):
+    """Groups at the least power of two and dy of subnormal numbers count at both tile sizes."""
+    k, n, d, out = size
+    gen = torch.Generator().manual_seed(13)
+    low, other = (2.0 ** -20, 1.0) if t == F16 else (2.0 ** -122, 2.0 ** 100)
+    for sx, sy in ((low, other), (other, low / 64)):
+        x, dy = rand(gen, k, n, d, std=sx, t=t), rand(gen, k, n, out, std=sy, t=t)
+        kept = cb.cb_ckpt_pack(x.cuda())
+        values = cb.cb_ckpt_unpack(kept).cpu()
+        dw = cb.cb_ckpt_wgrad(kept, dy.cuda())
+        for j in range(k):
+            close(f"dw[{j}]", dw[j], ref.wgrad(values[j], dy[j])["dw"])
+
+
 # --- together, streams, graphs ------------------------------------------------------
 
 def learner_step(x, o, wo, gate, post, pre, w, y):
@@ -714,6 +748,28 @@ def test_operators_together(t):
         close("h", h[j], f["y"])
         assert torch.equal(got["kept"][j].cpu().double(), ref.kept(h[j]))
         close("dwo", got["dwo"][j], ref.wgrad(ref.kept(o[j]), got["dblock"][j].cpu())["dw"])
+
+
+@pytest.mark.parametrize("t", TYPES, ids=str)
+def test_operators_together_gradients(t):
+    """The gradients of a step, each within its own bound of what the operator before it gave: dh of the loss, then
+    all five of the norm's, and the same values in the step as in calls one by one."""
+    a = step_inputs(t)
+    got, (xo, h, block) = learner_step(*a)
+    x, o, wo, gate, post, pre, w, y = a
+    _, lse = cb.cb_vocab_xent_fwd(h, w, y)
+    dh, dw = cb.cb_vocab_xent_bwd(h, w, y, lse, grad_scale=64.0)
+    g = cb.cb_gated_norm_bwd(xo, dh, block=block, gate=gate, gate_rows=8, res_scale=0.5, post=post, pre=pre)
+    assert set(g) == {"dx", "dblock", "dgate", "dpost", "dpre"} and torch.equal(dw, got["dw"])
+    for name in g:
+        assert torch.equal(g[name], got[name]), name
+    xo, h, block, dh, gate, post, pre, w, y = (v.cpu() for v in (xo, h, block, dh, gate, post, pre, w, y))
+    for j in range(2):
+        close("dh", dh[j], ref.xent(h[j], w[j], y[j], IGNORE, 64.0)["dh"])
+        want = ref.norm_bwd(xo[j], dh[j], None, block[j], gate[j], 8, 0.5, post[j], pre[j], float(torch.tensor(1e-5)))
+        assert set(want) == set(g)
+        for name in want:
+            close(f"{name}[{j}]", got[name][j], want[name])
 
 
 def test_operators_on_another_stream():
