@@ -949,3 +949,42 @@ def test_memory_of_a_given_stream():
     assert torch.cuda.current_stream().cuda_stream == torch.cuda.default_stream().cuda_stream
     torch.cuda.current_stream().wait_stream(s)
     assert all(torch.equal(a, b) for a, b in zip((*want, *grads), (loss, lse, dh, dw)))
+
+
+def test_given_stream_in_a_graph():
+    """Two calls beside each other in a graph, one on a stream that the caller forks and joins."""
+    k, n, d, v = 2, 40, 64, 900
+
+    def inputs(seed):
+        return [x.cuda() for x in (*xent_inputs(k, n, d, v, BF16, pad=0.2, seed=seed),
+                                   *xent_inputs(k, n, d, v, BF16, pad=0.4, seed=seed + 50))]
+
+    def step(a, side=None):
+        now = torch.cuda.current_stream()
+        if side is not None:
+            side.wait_stream(now)
+        other = cb.cb_vocab_xent_fwd(*a[3:], stream=side)
+        grads = cb.cb_vocab_xent_bwd(*a[3:], other[1], stream=side)
+        mine = cb.cb_vocab_xent_fwd(*a[:3])
+        mine_grads = cb.cb_vocab_xent_bwd(*a[:3], mine[1])
+        if side is not None:
+            now.wait_stream(side)
+        return (*other, *grads, *mine, *mine_grads)
+
+    a, side = inputs(1), torch.cuda.Stream()
+    step(a, side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(a, side)
+    for seed in (2, 3, 4, 5):
+        new = inputs(seed)
+        want = step(new)
+        for to, x in zip(a, new):
+            to.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want, got)), seed
+        eager = step(new, side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want, eager)), seed
