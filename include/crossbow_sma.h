@@ -397,7 +397,15 @@ int cb_test_conv_static(int k, int b, int Ci, int H, int W, int Co, int R, int s
  * that they can lie in flat parameter and gradient vectors.
  *   - type: CB_TYPE_*, the type of activations, weights, gates and their
  *     gradients.  Norm gammas and their gradients, losses and log-sum-exps
- *     are fp32.  Sums are fp32 or wider; each result is rounded once.
+ *     are fp32.  Sums are fp32 or wider and each result is rounded once; the
+ *     backward of the loss also rounds each logit's gradient to `type` (fp16:
+ *     2^14 times it) before the two products that it enters.
+ *   - Products of fp32 matrices are taken of three bf16 numbers a float, six
+ *     of the nine products: off by 2^-22 of a product at the most and mostly
+ *     by less than 2^-24.  Floats below 2^-110 are taken to 2^-134, and the
+ *     products of an infinity are NaN.
+ *   - Exponentials are the hardware's: exp(x) is off by (4 |x| + 16) 2^-24 of
+ *     itself at the most, and 0 below 2^-126.
  *   - Pointers are device memory of the device that is current at the call
  *     and that `stream` (a hipStream_t, NULL = the default stream) belongs
  *     to, aligned to their element; the workspace to 256 bytes, 8-bit
@@ -410,11 +418,12 @@ int cb_test_conv_static(int k, int b, int Ci, int H, int W, int Co, int R, int s
  *     into a graph.  Results do not depend on timing (no atomics).
  *   - CB_EINVAL for a description out of range, a NULL or misaligned
  *     pointer, CB_ENOMEM for a short workspace, CB_EDEVICE if a launch
- *     fails; cb_last_error(NULL) has the message. */
+ *     fails; cb_last_error(NULL) has the message.  After CB_EINVAL and
+ *     CB_ENOMEM nothing has been launched. */
 enum { CB_TYPE_FLOAT = 0, CB_TYPE_HALF = 1, CB_TYPE_BFLOAT = 2 };
 
 /* Softmax cross-entropy of the logits h W^T over v words, from the hidden
- * rows; logits are never stored.  A row whose label is `ignore` does not
+ * rows; the logits are not kept.  A row whose label is `ignore` does not
  * count: whatever h holds there (NaN too) has no effect, its lse is 0 and
  * its dh 0.  Any other label outside [0, v) makes the learner's loss NaN
  * and contributes no one-hot term, as in cb_step. */
@@ -433,9 +442,11 @@ typedef struct {
  * and the call refused, also where a launch could not hold its workgroups
  * (the forward from n * v of 2^38 on, in 16 bits 2^39).
  * The forward's holds the counted rows and one pair of floats for each row
- * and 128 or 256 words; the backward's also the logit gradients of one piece
+ * and 16 to 256 words; the backward's also the logit gradients of one piece
  * of the vocabulary (128 MB or 4096 words, whichever is more) and fp32 sums
- * of dh.  Where rows of w do not start on 16 bytes it holds a copy of w. */
+ * of dh.  Where few tiles share long sums both hold the shares' sums, logits
+ * among them, of 64 MB at the most.  Where rows of w do not start on 16 bytes
+ * they hold a copy of w. */
 size_t cb_vocab_xent_workspace_bytes(const cb_vocab_xent* x, int backward);
 
 /* loss [k]: the mean over each learner's counted rows of

@@ -553,8 +553,9 @@ def cb_vocab_xent_fwd(h, w, labels, ignore=-100, workspace=None, stream=None):
 def cb_vocab_xent_bwd(h, w, labels, lse, grad_scale=1.0, ignore=-100, dw=None, workspace=None,
                       stream=None):
     """The gradients of grad_scale * loss of cb_vocab_xent_fwd, given its lse:
-    (dh [k, n, d], dw [k, v, d]) in the inputs' type.  dw may be given, for
-    instance as a view of a flat gradient vector; it is overwritten."""
+    (dh [k, n, d], dw [k, v, d]) in the inputs' type, which also holds the logits'
+    gradients on the way.  dw may be given, for instance as a view of a flat gradient
+    vector; it is overwritten."""
     who = "cb_vocab_xent_bwd"
     L = lib()
     x = _xent(who, h, w, labels, ignore)

@@ -13,11 +13,12 @@
 // columns a thread, one step ahead into registers, converted and written to
 // LDS in the layout that dy's loads have there.  One launch, and for fp32
 // three MFMAs a product instead of six: x is one bf16 number, dy three.
-//   Large layers (tiles of 256; 8192 rows, 2048 x 8192, bf16: 1,280 TFLOP/s):
-// x is unpacked once into the workspace, and the tiles take both operands
-// straight to LDS.  Converting in every one of the out/256 workgroups that
-// read a tile of x costs more (240 us there against 216 us and 11 us for the
-// unpacking).
+//   Large layers (tiles of 256; 8192 rows, 2048 x 8192, bf16: 197 us in the
+// long run, 1,390 TFLOP/s, and 222 to 267 us in the first milliseconds under
+// load, when the card's clock is lower): x is unpacked once into the
+// workspace, and the tiles take both operands straight to LDS.  Converting in
+// every one of the out/256 workgroups that read a tile of x costs more (240 us
+// there against 216 us and 11 us for the unpacking, side by side).
 //   Where the tiles do not fill the CUs, or the last round of them leaves most
 // idle, that round's tiles are shared by workgroups that take some of the rows
 // each, and kept_grad_join adds their sums in order.

@@ -20,8 +20,13 @@
 // the backward pass the three column sums do too; each worker leaves one row
 // of partial sums, which norm_sums adds in a fixed order.  Workers are laid
 // out so that none has rows of two gate rows unless it has all rows of each.
-// 16,384 rows of 4096, bf16: forward 106 us (5.1 TB/s of the four tensors that
-// it moves), backward 178 us (4.5 TB/s of six) and 10 us for the column sums.
+// 16,384 rows of 4096, bf16: forward 104 us (5.2 TB/s of the four tensors that
+// it moves; 129 us a call with the 8-bit form of y, where packing y in a call
+// of its own takes 33 more), backward 174 us (4.6 TB/s of six) and 9 us for the
+// column sums.  8192 rows of 4096, fp32: 110 and 169 us a call (4.9 and 4.8
+// TB/s).  Two sizes stay far from that: some thousand rows, where every worker
+// has one row and its partial sums are as much again (2 x 1000 x 1001, fp16:
+// 13 and 6 us, the tensors alone would take 6), and workers of 1024 threads.
 #include "kept.hpp"
 
 #include <algorithm>
@@ -40,7 +45,12 @@ struct Split {
 // The shape of a worker for rows of d: TPR threads of U * 8 columns.  Of the
 // 16-bit types a thread takes two eights from 512 columns on: the backward
 // kernel's registers allow two waves a SIMD either way, and twice as much is
-// in flight; of fp32, which would spill, only above 8192.
+// in flight; of fp32, which would spill, only above 8192.  1024 threads leave a
+// lane 128 registers, which the backward passes: fp32 spills 41 (d a multiple
+// of 8) to 74 registers from 4097 columns on, 405 to 572 above 8192, fp16
+// there 209 to 276 and bf16 349 to 423 (4096 rows, backward: fp32 of 8192
+// columns 366 us, 2.2 TB/s; of 16,384 columns fp32 1520, fp16 965 and bf16 1185
+// us, 0.7 to 1.1 TB/s).
 struct Shape {
   int tpr, u;
 };

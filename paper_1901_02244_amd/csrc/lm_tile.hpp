@@ -12,7 +12,8 @@
 // largest are taken, which leaves out at most 2^-22 of the product (two of 2^-7
 // times 2^-16) and mostly less than fp32's own rounding of it, 2^-24.  The
 // split is made in registers on the way from LDS.
-// (An infinity splits into an infinity and NaNs: its products are NaN.)
+// (An infinity splits into an infinity and NaNs: its products are NaN.  bf16
+// ends at 2^-133, so that floats below 2^-110 are taken to 2^-134.)
 //
 // A step takes 128 bytes of contraction per row (64 elements of 16 bits or 32
 // floats) from global memory straight into LDS (buffer loads with the LDS as

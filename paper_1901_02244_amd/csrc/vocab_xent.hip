@@ -1,5 +1,5 @@
 // vocab_xent.hip -- softmax cross-entropy of a projection onto a large
-// vocabulary, and its gradient, without the logits ever being kept.
+// vocabulary, and its gradient, without keeping the logits.
 //
 // For the counted rows r (label not `ignore`) of a learner, C of them:
 //   l[r][v] = sum_d h[r][d] W[v][d]        lse[r] = log sum_v exp l[r][v]
@@ -12,7 +12,10 @@
 // product with vocabulary tiles as P and rows as Q leaves a row's logits of
 // one tile in few lanes, which reduce them to a (max, sum of exponentials)
 // per tile (xent_logits); xent_join_* joins those and xent_mean takes the
-// mean.  Backward: for each piece of the vocabulary the
+// mean.  Where the tiles are too few for the card and the sums long, several
+// workgroups share a tile's sum, and what they leave in the workspace are
+// logits after all: fp32 ones, 64 MB of shares at the most, which
+// xent_sums_loss and xent_sums_grad add up.  Backward: for each piece of the vocabulary the
 // logits are computed again, g of the piece is stored in the input type, and
 // two products add its share of dh (fp32 sums across pieces) and write its
 // rows of dW; the last piece's product writes dh itself, or, where few tiles
@@ -22,7 +25,12 @@
 // g is stored times 2^14 in fp16, so that probabilities down to 2^-28 are
 // normal numbers and -1 is still in range; the scale is taken out, with s/C,
 // from the fp32 sums.  That store is the only rounding before the results'
-// own.
+// own: the products run on 16-bit operands, and g in fp32 would take three
+// times the matrix instructions.  Against 64 bits it moves the error of dh and
+// dW, most of it their own rounding, from 2.1e-4 to 2.5e-4 of their norm in
+// fp16 (two learners of 1023 rows) and from 1.7e-3 to 1.8e-3 in bf16 (8192
+// rows).  Exponentials are the hardware's exp2 of a rounded product: off by
+// (4 |x| + 16) 2^-24 at the most, 0 below 2^-126.
 //
 // Many rows are bound by the matrix cores (bf16, 8192 rows, about 7400 of
 // them counted, 4096 wide, 128,000 words, both passes: 25.3 ms, 1,220 TFLOP/s of
