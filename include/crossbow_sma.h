@@ -440,7 +440,7 @@ typedef struct {
 
 /* Workspace of the forward, or with backward != 0 of the backward call; 0,
  * and the call refused, also where a launch could not hold its workgroups
- * (the forward from n * v of 2^38 on, in 16 bits 2^39).
+ * (2^29 rows of a learner; gradients of some 10^7 tiles).
  * The forward's holds the counted rows and one pair of floats for each row
  * and 16 to 256 words; the backward's also the logit gradients of one piece
  * of the vocabulary (128 MB or 4096 words, whichever is more) and fp32 sums

@@ -473,7 +473,7 @@ using ThinTile = Tile<T, PC, QC, 256, THIN_Q, 4, 1>;
 
 // Whether the first axis of a grid holds these workgroups: its threads are a
 // 32-bit number.
-inline bool launch_holds(int64_t workgroups, int threads) {
+constexpr bool launch_holds(int64_t workgroups, int threads) {
   return workgroups <= UINT32_MAX / threads;
 }
 

@@ -187,13 +187,11 @@ Layout layout(const XentArgs& a, bool backward) {
     l.rloss = take((int64_t)k * n * 4);
     l.means = n > MANY ? take(up(n, CHUNK) / CHUNK * k * 16) : 0;
   }
-  // the gathering of the rows, the logits, and for whole pieces and the last
-  // one logits and gradients; the other launches have a bounded grid
+  // the gathering of the rows, and for whole pieces and the last one logits and
+  // gradients; the loss's tiles take several launches if need be, and the other
+  // launches have a bounded grid
   bool fits = n <= MANY || launch_holds(up(n, 32) / 32, 256);
-  if (!backward) {
-    const int64_t words = l.logits.shape == THIN ? (int64_t)l.parts * 256 : v;
-    fits &= launch_holds(tiles_of(l.logits.shape, 1, words, n), threads_of(l.logits.shape));
-  } else {
+  if (backward) {
     for (const int64_t vn : {std::min(l.piece, v), (v - 1) % l.piece + 1}) {
       const int shape = plan_logits(a.type, k, n, d, (int)vn).shape;
       fits &= launch_holds(tiles_of(shape, 1, vn, n), threads_of(shape)) &&
@@ -358,6 +356,7 @@ struct LogitArgs {
   const int *lab, *row;
   int ldlab;        // labels of a learner apart
   // forward
+  int first;        // the launch's first tile
   float2* part;     // [k][parts][cap]
   float* plog;      // [k][cap]
   int parts, words;
@@ -464,10 +463,11 @@ __global__ __launch_bounds__(TL::THREADS, 2) void xent_logits(LogitArgs args) {
   }
   // the counted rows' tiles, first of a grid for all rows
   const int words = MODE == LOSS ? a.words : TL::BP;
+  const int tile = (MODE == LOSS ? a.first : 0) + blockIdx.x;
   const int np = (a.vn + words - 1) / words, nq = (cnt + TL::BQ - 1) / TL::BQ;
-  if (a.vn <= 0 || (int)blockIdx.x >= np * nq) return;
+  if (a.vn <= 0 || tile >= np * nq) return;
   int tp, tq;
-  tile_of<8>(blockIdx.x, np, nq, tp, tq);
+  tile_of<8>(tile, np, nq, tp, tq);
   const int p0 = tp * words, q0 = tq * TL::BQ;
   if constexpr (MODE == LOSS) a.vn = min(a.vn, p0 + words);
   const Operand<T> W{(const T*)a.w + j * a.pstride, a.ldw, a.vn, a.d};
@@ -936,6 +936,22 @@ __global__ __launch_bounds__(256) void xent_dw_join(DwArgs a, int splits) {
 
 // --- launches ----------------------------------------------------------------------
 
+// The tiles of the loss, in as many launches as their grids need.
+template <class TL>
+hipError_t launch_loss(LogitArgs a, int64_t v, int n, int k, hipStream_t s) {
+  constexpr int64_t MOST = UINT32_MAX / TL::THREADS / NXCD * NXCD;
+  static_assert(launch_holds(MOST, TL::THREADS));
+  const int64_t all = tiles(v, n, TL::BP, TL::BQ);
+  for (int64_t first = 0; first < all; first += MOST) {
+    a.first = (int)first;
+    const dim3 grid((unsigned)std::min(MOST, all - first), k);
+    if (hipError_t e =
+            launch_with_lds<TL::LDS, xent_logits<TL, LOSS>>(grid, TL::THREADS, s, a))
+      return e;
+  }
+  return hipSuccess;
+}
+
 template <class T, int MODE>
 hipError_t launch_logits(const LogitArgs& a, Plan p, int k, int n, hipStream_t s) {
   using Big = BigTile<T, false, false>;
@@ -945,11 +961,18 @@ hipError_t launch_logits(const LogitArgs& a, Plan p, int k, int n, hipStream_t s
                 Thin::THREADS == threads_of(THIN));
   static_assert(Big::BP == bp_of(BIG) && Big::BQ == bq_of(BIG) && Mid::BP == bp_of(MID) &&
                 Mid::BQ == bq_of(MID) && Thin::BP == bp_of(THIN) && Thin::BQ == bq_of(THIN));
-  if constexpr (sizeof(T) == 2 && MODE != SUMS)
-    if (p.shape == BIG) return launch_tile<Big, xent_logits<Big, MODE>>(a.vn, n, k, p.splits, s, a);
-  if (p.shape == MID) return launch_tile<Mid, xent_logits<Mid, MODE>>(a.vn, n, k, p.splits, s, a);
-  const int64_t v = MODE == LOSS ? (int64_t)a.parts * Thin::BP : a.vn;
-  return launch_tile<Thin, xent_logits<Thin, MODE>>(v, n, k, p.splits, s, a);
+  if constexpr (MODE == LOSS) {
+    if constexpr (sizeof(T) == 2)
+      if (p.shape == BIG) return launch_loss<Big>(a, a.vn, n, k, s);
+    if (p.shape == MID) return launch_loss<Mid>(a, a.vn, n, k, s);
+    return launch_loss<Thin>(a, (int64_t)a.parts * Thin::BP, n, k, s);
+  } else {
+    if constexpr (sizeof(T) == 2 && MODE != SUMS)
+      if (p.shape == BIG)
+        return launch_tile<Big, xent_logits<Big, MODE>>(a.vn, n, k, p.splits, s, a);
+    if (p.shape == MID) return launch_tile<Mid, xent_logits<Mid, MODE>>(a.vn, n, k, p.splits, s, a);
+    return launch_tile<Thin, xent_logits<Thin, MODE>>(a.vn, n, k, p.splits, s, a);
+  }
 }
 
 template <class TLH, class TLW>

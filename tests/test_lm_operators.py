@@ -176,6 +176,28 @@ def test_xent_few_counted_rows_of_many_words(t):
     assert (dh == 0).all()
 
 
+@pytest.mark.parametrize("t", [F32, BF16], ids=str)
+def test_xent_of_more_tiles_than_a_launch_holds(t):
+    """Two million rows (fp32; four in 16 bits) of 131,075 words: 2^24 tiles of 256 threads and some more (2^23 of
+    512), past what one grid holds.  All words but 16 are zero; those lie at both ends."""
+    n, d, v = (2 ** 21 if t == F32 else 2 ** 22) + 300, 8, 2 ** 17 + 3
+    gen = torch.Generator("cuda").manual_seed(21)
+    some = torch.cat([torch.arange(8), v - 8 + torch.arange(8)]).cuda()
+    w = torch.zeros(1, v, d, dtype=t, device="cuda")
+    w[0, some] = torch.randn(16, d, generator=gen, device="cuda").to(t)
+    h = torch.randn(1, n, d, generator=gen, device="cuda").to(t)
+    y = some[torch.randint(0, 16, (1, n), generator=gen, device="cuda")].int()
+    loss, lse = cb.cb_vocab_xent_fwd(h, w, y)
+    logits = h[0].double() @ w[0, some].double().t().contiguous()
+    want = torch.log((v - 16) + logits.exp().sum(1))
+    # sums of 131,075 terms in fp32, tile by tile, 20 roundings deep at the most, of logits that are off by el
+    el = (d + 32) * ref.U * (h[0].double().abs() @ w[0, some].double().abs().t().contiguous()).amax(1)
+    assert ((lse[0].double() - want).abs() < 1e-5 + 2 * el).all()
+    hit = torch.where(y[0] < 8, y[0], y[0] - (v - 16)).long()
+    rows = want - logits.gather(1, hit[:, None])[:, 0]
+    assert abs(loss[0].item() - rows.mean().item()) < 1e-5 + 4 * el.mean().item()
+
+
 @pytest.mark.parametrize("t", TYPES, ids=str)
 def test_xent_label_out_of_range(t):
     """As in cb_step: the learner's loss is NaN, the gradient has no one-hot term."""
