@@ -15,12 +15,12 @@
 // mean.  Where the tiles are too few for the card and the sums long, several
 // workgroups share a tile's sum, and what they leave in the workspace are
 // logits after all: fp32 ones, 64 MB of shares at the most, which
-// xent_sums_loss and xent_sums_grad add up.  Backward: for each piece of the vocabulary the
-// logits are computed again, g of the piece is stored in the input type, and
-// two products add its share of dh (fp32 sums across pieces) and write its
-// rows of dW; the last piece's product writes dh itself, or, where few tiles
-// share a long vocabulary in splits, xent_dh adds them up.  Every sum runs in
-// a fixed order.
+// xent_sums_loss and xent_sums_grad add up.  Backward: for each piece of the
+// vocabulary the logits are computed again, g of the piece is stored in the
+// input type, and two products add its share of dh (fp32 sums across pieces)
+// and write its rows of dW; the last piece's product writes dh itself, or,
+// where few tiles share a long vocabulary in splits, xent_dh adds them up.
+// Every sum runs in a fixed order.
 //
 // g is stored times 2^14 in fp16, so that probabilities down to 2^-28 are
 // normal numbers and -1 is still in range; the scale is taken out, with s/C,
