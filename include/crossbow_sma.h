@@ -567,8 +567,10 @@ int cb_embed_bwd(const cb_embed* e, const void* dy, void* dw, int64_t dstride, i
  *     alone); they are constants and get no gradient.  Larger ones grow with
  *     the sequence until fp32 overflows.
  *   - states are [k][seqs][heads][dk][dv], fp32; NULL for zeros, or where the
- *     last is not wanted (in 16-bit types results may then differ by 2^-15 of
- *     their terms' magnitudes, before they are rounded).  A sequence without rows hands on what it was given. */
+ *     last is not wanted.  A sequence without rows hands on what it was given.
+ *   - in 16-bit types results may be off by 2^-16 of their terms' magnitudes
+ *     before they are rounded, and where no state (backward: no dstate_in) is
+ *     wanted by 2^-15. */
 typedef struct {
   int32_t type;
   int32_t k, n, seqs;        /* k*n <= 2^30, k*seqs*heads <= 2^20 */

@@ -30,12 +30,13 @@
 // and without fp16's range for scores and states) or three (fp32). Weights,
 // states and scores are fp32; c times its weight enters the state's sum as
 // three bf16 numbers, which is all of it, so that states are as good as fp32
-// sums (in 16-bit types two for a call that returns no state: 2^-17 is left
-// out; bf16, four sequences of 2048, 32 heads of 128: 98 us instead of 112,
-// backward 213 instead of 229). States and scores enter the result's
-// products as three in fp32, else as two, which leaves out 2^-17 of them, far
-// below the result's own rounding (2^-9, 2^-12). One would leave an error as
-// large as that rounding (176 us instead of 213).
+// sums (in 16-bit types two for a call that returns no state: up to 2^-16 is
+// left out; bf16, four sequences of 2048, 32 heads of 128: 98 us instead of
+// 112, backward 213 instead of 229). States and scores enter the result's
+// products as three in fp32, else as two, which leaves out up to 2^-16 of them,
+// far below the result's own rounding (2^-9, 2^-12). One would leave an error
+// as large as that rounding (176 us instead of 213). Where both operands have
+// two parts (fp16) all four products are taken.
 //
 // Few sequences and heads leave CUs idle, and a sequence is then cut into
 // segments: a first pass leaves each segment's own state, attn_scan goes over
@@ -203,10 +204,13 @@ __device__ __forceinline__ Parts<N> parts_of(const float (&v)[8]) {
   }
   return r;
 }
-// The largest products of two sums, the smallest of them first.
+// The products of two sums, the smallest of them first; where an operand has
+// three parts, without those that are 2^-22 of the whole or less. (The product
+// of two second parts is not one of them: the first part is cut off, so that
+// the second can be 2^-7 of the number and always has its sign.)
 template <int NA, int NB>
 __device__ __forceinline__ f32x4 mul(const Parts<NA>& a, const Parts<NB>& b, f32x4 c) {
-  constexpr int M = (NA > NB ? NA : NB) - 1;
+  constexpr int M = NA == 2 && NB == 2 ? 2 : (NA > NB ? NA : NB) - 1;
 #pragma unroll
   for (int sum = M; sum >= 0; --sum)
 #pragma unroll
