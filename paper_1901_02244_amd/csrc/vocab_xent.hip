@@ -415,15 +415,16 @@ __global__ __launch_bounds__(1024) void distill_rows(TeacherArgs a) {
       const int w = a.words[at + i];
       const bool in = w >= 0 && t != NEG_INF;
       word[i] = in ? w : -1;
-      share[i] = in ? t * a.factor : NEG_INF;
+      share[i] = in ? t : NEG_INF;
       if (in) top = fmaxf(top, share[i]);
     }
     top = all_of(top, joined, [](float x, float y) { return fmaxf(x, y); });
-    // NaN logits have no maximum: they count all the same
+    // (The maximum goes off before the factor: t / T may pass fp32's largest
+    // value.  NaN logits have no maximum: they count all the same.)
     float sum = 0.f, some = 0.f;
     for (int i = tid; i < a.m; i += all) {
       const bool in = word[i] >= 0;
-      const float e = in ? expf(share[i] - top) : 0.f;
+      const float e = in ? expf((share[i] - top) * a.factor) : 0.f;
       share[i] = e;
       sum += e;
       some += in;

@@ -1,9 +1,10 @@
 """Where the sequence operators meet their documented bounds (GPU): operands whose
-low bits all count."""
+low bits all count, teachers at the ends of fp32."""
 import pytest
 
+import lm_seq_oracle as ref
 import paper_1901_02244_amd as cb
-from test_lm_seq_operators import BF16, F16, close
+from test_lm_seq_operators import BF16, F16, F32, TYPES, close, distill_inputs
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -61,3 +62,31 @@ def test_attn_every_part_of_an_operand_counts(states, rows, t):
     bound = size * (2.0 ** (-16 if states else -15) + 4 * (n + 8) * U) + torch.finfo(t).eps / 2 * want.abs()
     for name, x in got.items():
         close(name, x[:, rows, 0], (want[:, None].expand(k, 8), bound[:, None].expand(k, 8)))
+
+
+# --- distillation ---------------------------------------------------------------
+
+@pytest.mark.parametrize("t", TYPES, ids=str)
+@pytest.mark.parametrize("temp", [0.5, 1.0, 4.0])
+def test_distill_teachers_at_the_ends_of_fp32(temp, t):
+    """Logits masked with fp32's lowest value, or at its largest: shares depend on differences only, so rows of them
+    alone are rows of equal logits, and beside others the lowest have none."""
+    h, w, words, teacher = distill_inputs(2, 40, 32, 60, 6, t)
+    words = words.abs()
+    low, high = torch.finfo(F32).min, torch.finfo(F32).max
+    ends, plain = teacher.clone(), teacher.clone()
+    ends[:, 0::4], plain[:, 0::4] = low, 0.0
+    ends[:, 1::4], plain[:, 1::4] = high, 0.0
+    ends[:, 2::4, 1:4], plain[:, 2::4, 1:4] = low, -1e5
+    ends[:, 3::4, 2], plain[:, 3::4, 2] = high, 1e5
+    what = (h.cuda(), w.cuda(), words.cuda())
+    results = []
+    for x in (ends, plain):
+        loss, lse, picked = cb.cb_vocab_distill_fwd(*what, x.cuda(), temperature=temp)
+        results.append((loss, lse, picked, *cb.cb_vocab_distill_bwd(*what, x.cuda(), lse, picked, temperature=temp)))
+    for a, b in zip(*results):
+        assert a.isfinite().all() and torch.equal(a, b)
+    for j in range(2):
+        want = ref.distill(h[j], w[j], words[j], plain[j], temp, 1.0)
+        for name, got in zip(("loss", "lse", "picked", "dh", "dw"), results[0]):
+            close(name, got[j], want[name])
