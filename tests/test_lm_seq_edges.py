@@ -1,10 +1,10 @@
 """Where the sequence operators meet their documented bounds (GPU): operands whose
-low bits all count, teachers at the ends of fp32."""
+low bits all count, teachers at the ends of fp32, words that most of a batch holds."""
 import pytest
 
 import lm_seq_oracle as ref
 import paper_1901_02244_amd as cb
-from test_lm_seq_operators import BF16, F16, F32, TYPES, close, distill_inputs
+from test_lm_seq_operators import BF16, F16, F32, I32, TYPES, close, distill_inputs, rand
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -90,3 +90,53 @@ def test_distill_teachers_at_the_ends_of_fp32(temp, t):
         want = ref.distill(h[j], w[j], words[j], plain[j], temp, 1.0)
         for name, got in zip(("loss", "lse", "picked", "dh", "dw"), results[0]):
             close(name, got[j], want[name])
+
+
+# --- embedding ------------------------------------------------------------------
+
+def pass_us(f):
+    """Median time of f in a graph."""
+    f()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        f()
+    times = []
+    for _ in range(9):
+        a, b = torch.cuda.Event(True), torch.cuda.Event(True)
+        a.record()
+        for _ in range(4):
+            graph.replay()
+        b.record()
+        torch.cuda.synchronize()
+        times.append(a.elapsed_time(b) * 250)
+    return sorted(times)[4]
+
+
+def test_embed_zeros_take_no_longer_for_frequent_words():
+    """The zeros of few words are a handful of stores, however often the words occur: a call that writes them takes
+    less than twice one that adds to a gradient and writes none."""
+    gen = torch.Generator().manual_seed(1)
+    n, d, v = 1 << 20, 8, 64
+    tok, dy = torch.randint(0, v - 1, (1, n), generator=gen, dtype=I32).cuda(), rand(gen, 1, n, d).cuda()
+    dw = torch.zeros(1, v, d, device="cuda")
+    zeros = pass_us(lambda: cb.cb_embed_bwd(dy, tok, dw=dw))
+    assert (dw[0, v - 1] == 0).all()
+    adds = pass_us(lambda: cb.cb_embed_bwd(dy, tok, dw=dw, accumulate=True))
+    assert zeros < 2 * adds, (zeros, adds)
+
+
+@pytest.mark.parametrize("t", TYPES, ids=str)
+@pytest.mark.parametrize("v", [3, 64, 65, 200])
+def test_embed_frequent_words_beside_words_that_no_token_names(v, t):
+    """A stretch of words whose tokens are more than one step of the search, with gaps before, between and behind; a
+    learner whose every token is the last word, one whose every token is the first."""
+    gen = torch.Generator().manual_seed(v)
+    n, d = 3000, 8
+    tok = (torch.randint(0, (v + 2) // 3, (4, n), generator=gen) * 3).clamp(max=v - 1).to(I32)
+    tok[1], tok[2] = v - 1, 0
+    tok[3, 1500:] = -100
+    dy = rand(gen, 4, n, d, t=t)
+    dw = cb.cb_embed_bwd(dy.cuda(), tok.cuda(), v)
+    for j in range(4):
+        close(f"dw[{j}]", dw[j], ref.embed_bwd(dy[j], tok[j], v, 1.0, -100))
