@@ -585,8 +585,9 @@ typedef struct {
 } cb_decay_attn;
 
 /* Workspace: the states of segments, where sequences and heads are few and
- * sequences are cut to fill the card (70 MB at the most), and backward
- * with shared key heads fp32 shares of dkey and dval for every head. */
+ * sequences are cut to fill the card (34 MB at the most; with starts 68 MB,
+ * and 20 bytes for every sequence), and backward with shared key heads fp32
+ * shares of dkey and dval for every head. */
 size_t cb_decay_attn_workspace_bytes(const cb_decay_attn* x, int backward);
 
 /* o [k*n][heads][dv]; state_out must not be state. */
