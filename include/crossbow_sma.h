@@ -628,7 +628,7 @@ typedef struct {
   const float* teacher;  /* [k*n][m] */
 } cb_vocab_distill;
 
-/* Workspace, as of cb_vocab_xent, and 4 bytes (backward: 8 m more) a row. */
+/* Workspace, as of cb_vocab_xent, and 8 bytes a row (backward: 4 + 8 m). */
 size_t cb_vocab_distill_workspace_bytes(const cb_vocab_distill* x, int backward);
 
 /* loss [k] (0 if no row counts); lse [k*n]: log sum exp of l; picked

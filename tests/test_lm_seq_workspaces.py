@@ -6,7 +6,7 @@ import itertools
 import pytest
 
 import paper_1901_02244_amd as cb
-from test_lm_seq_boundary import attn
+from test_lm_seq_boundary import attn, described, distill
 
 
 def attn_bytes(backward, **kw):
@@ -40,3 +40,15 @@ def test_attn_workspace_of_the_most_sequences():
     need = attn_bytes(0, k=1, n=1 << 20, seqs=1 << 20, heads=1, kv_heads=1, dk=128, dv=128, ldq=128, ldk=128, ldv=128,
                       decay_stride=1, starts=1 << 40)
     assert 70_000_000 < need <= 68_000_000 + (20 << 20)
+
+
+@pytest.mark.parametrize("k, n, m", [(1, 8192, 64), (3, 1000, 1), (8, 16, 1024)])
+def test_distill_workspace_is_the_losss_and_the_lists(k, n, m):
+    """8 bytes a row beside the loss of labels, backward 4 and 8 for every entry, each array up to 256 bytes."""
+    L, d, v = cb.lib(), 64, 1000
+    size = dict(type=2, k=k, n=n, d=d, v=v, h=1 << 40, ldh=d, w=1 << 40, pstride=v * d)
+    x = described(cb.cb_vocab_xent, dict(size, ignore=0, labels=1 << 40), {})
+    for back, arrays in ((0, [4, 4]), (1, [4, 4 * m, 4 * m])):
+        a = L.cb_vocab_xent_workspace_bytes(ctypes.byref(x), back)
+        b = L.cb_vocab_distill_workspace_bytes(ctypes.byref(distill(**size, m=m)), back)
+        assert b - a == sum((k * n * each + 255) // 256 * 256 for each in arrays)
