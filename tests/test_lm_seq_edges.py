@@ -1,10 +1,12 @@
 """Where the sequence operators meet their documented bounds (GPU): operands whose
-low bits all count, teachers at the ends of fp32, words that most of a batch holds."""
+low bits all count, teachers at the ends of fp32, sequences cut in many segments
+at every width, words that most of a batch holds."""
 import pytest
 
 import lm_seq_oracle as ref
 import paper_1901_02244_amd as cb
-from test_lm_seq_operators import BF16, F16, F32, I32, TYPES, close, distill_inputs, rand
+from test_lm_seq_operators import (BF16, F16, F32, I32, TYPES, attn_check, attn_inputs, close, distill_check,
+                                   distill_inputs, rand)
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -64,6 +66,20 @@ def test_attn_every_part_of_an_operand_counts(states, rows, t):
         close(name, x[:, rows, 0], (want[:, None].expand(k, 8), bound[:, None].expand(k, 8)))
 
 
+@pytest.mark.parametrize("t", TYPES, ids=str)
+@pytest.mark.parametrize("width", [(128, 128), (96, 128), (256, 256), (130, 200)], ids=str)
+def test_attn_uneven_sequences_in_many_segments(width, t):
+    """Uneven sequences of three to nine segments, whose states are carried from one to the next, for heads past 64
+    and past 128 columns."""
+    k, n, heads = 2, 1300, 2
+    q, key, val, decay, dout, gen = attn_inputs(k, n, heads, 1, *width, t, fused=True)
+    decay = decay * 0.02  # a segment's state reaches over the next ones
+    starts = torch.tensor([[0, 3, 40, 1200, 1290], [10, 10, 500, 501, 1300]], dtype=I32)
+    state, dstate = rand(gen, k, 4, heads, *width), rand(gen, k, 4, heads, *width)
+    attn_check(q, key, val, decay, dout, scale=1.0 / 16, starts=starts, state=state, dstate=dstate)
+    attn_check(q, key, val, decay, dout, scale=1.0 / 16, starts=starts)
+
+
 # --- distillation ---------------------------------------------------------------
 
 @pytest.mark.parametrize("t", TYPES, ids=str)
@@ -90,6 +106,29 @@ def test_distill_teachers_at_the_ends_of_fp32(temp, t):
         want = ref.distill(h[j], w[j], words[j], plain[j], temp, 1.0)
         for name, got in zip(("loss", "lse", "picked", "dh", "dw"), results[0]):
             close(name, got[j], want[name])
+
+
+@pytest.mark.parametrize("t", TYPES, ids=str)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_distill_teachers_without_a_softmax(bad, t):
+    """A logit that counts and is NaN or infinite: the learner's loss, its row's dh and its words' dW are NaN, also
+    where all of a row's logits are; nothing else is."""
+    h, w, words, teacher = distill_inputs(3, 40, 32, 4000, 6, t)
+    teacher[0, 3, 2], words[0, 3, 2] = bad, 17
+    teacher[2, 5], words[2, 5, 0] = bad, 3
+    words[2, 5, 1:] = -1
+    loss, *_ = distill_check(h, w, words, teacher)
+    assert loss[0].isnan() and not loss[1].isnan() and loss[2].isnan()
+
+
+def test_distill_repeats_bit_for_bit():
+    h, w, words, teacher = (x.cuda() for x in distill_inputs(2, 300, 96, 3000, 9, BF16))
+    first = None
+    for _ in range(3):
+        loss, lse, picked = cb.cb_vocab_distill_fwd(h, w, words, teacher, temperature=2.0)
+        got = [loss, lse, picked, *cb.cb_vocab_distill_bwd(h, w, words, teacher, lse, picked, temperature=2.0)]
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(got, first))
 
 
 # --- embedding ------------------------------------------------------------------
