@@ -31,12 +31,13 @@
 // states and scores are fp32; c times its weight enters the state's sum as
 // three bf16 numbers, which is all of it, so that states are as good as fp32
 // sums (in 16-bit types two for a call that returns no state: up to 2^-16 is
-// left out; bf16, four sequences of 2048, 32 heads of 128: 98 us instead of
-// 112, backward 213 instead of 229). States and scores enter the result's
+// left out; bf16, four sequences of 2048, 32 heads of 128: 106 us instead of
+// 122, backward 214 instead of 247). States and scores enter the result's
 // products as three in fp32, else as two, which leaves out up to 2^-16 of them,
 // far below the result's own rounding (2^-9, 2^-12). One would leave an error
 // as large as that rounding (176 us instead of 213). Where both operands have
-// two parts (fp16) all four products are taken.
+// two parts all four products are taken (fp16, as above: 175 us, and 164 with
+// three, which left out 2^-14 of a term).
 //
 // Few sequences and heads leave CUs idle, and a sequence is then cut into
 // segments: a first pass leaves each segment's own state, attn_scan goes over

@@ -10,12 +10,12 @@
 // batch holds has as many threads as others; a run that passes a piece's end
 // leaves fp32 partial sums, which embed_join adds in order, a workgroup a run
 // (fp32, 65,536 rows of 64: 53 us for the rows of 64 words, 160 for those of a
-// single one, of which 100 join its 1024 pieces).  Rows of words
+// single one, of which 123 join its 1024 pieces).  Rows of words
 // that no token names are zeros, written in the same launch by workgroups of
 // their own, which find out which words of theirs are named: the sums wait for
 // memory's answers while those keep it busy (bf16, 16,384 tokens, 128,000 words
 // of 4096: 217 us for both, 5.4 TB/s; zeros during the sort and the sums behind
-// it: 194 and 71), in a time that does not depend on how often (fp32, 65,536
+// it: 194 and 71), in a time that hardly depends on how often (fp32, 65,536
 // rows of 64, 64 words: 53 us, 47 without zeros, and 208 where a workgroup
 // walked the tokens of its words).  Lookup and gradient together: 296 us, 4.9 TB/s.
 #include "kept.hpp"

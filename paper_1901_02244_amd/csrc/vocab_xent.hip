@@ -32,6 +32,10 @@
 // the loss's, with a factor before the exponentials, but for g at the
 // teacher's words: distill_fix stores p - q there, from the forward's logits
 // and with one rounding, over the p that the tiles have left.
+// Each entry of a row's list is compared with every other one, to add the
+// shares of a word that is named twice: fp32, 8192 rows of 64, 1024 words, both
+// passes of distill_rows take 146 us with 64 entries, 544 with 256 and 5,810
+// with 1024 (the whole step 255, 662 and 5,950).
 //
 // g is stored times 2^14 in fp16, so that probabilities down to 2^-28 are
 // normal numbers and -1 is still in range; the scale is taken out, with s/C,
@@ -40,7 +44,8 @@
 // times the matrix instructions.  Against 64 bits it moves the error of dh and
 // dW, most of it their own rounding, from 2.1e-4 to 2.5e-4 of their norm in
 // fp16 (two learners of 1023 rows) and from 1.7e-3 to 1.8e-3 in bf16 (8192
-// rows).  Exponentials are the hardware's exp2 of a rounded product: off by
+// rows); from a teacher, where many entries of g count instead of one that is
+// next to -1, to 2.9e-4 and 2.3e-3.  Exponentials are the hardware's exp2 of a rounded product: off by
 // (4 |x| + 16) 2^-24 at the most, 0 below 2^-126.
 //
 // Many rows are bound by the matrix cores (bf16, 8192 rows, about 7400 of
